@@ -61,13 +61,13 @@ typedef enum {
     WFQ_ERR_SCRATCH_TOO_SMALL = 7 /* beyond the size limit of wfq_quantize_filters_static */
 } wfq_status_t;
 
-typedef enum { WFQ_F32 = 0, WFQ_F16 = 1, WFQ_BF16 = 2 /* output only */ } wfq_dtype_t;
+typedef enum { WFQ_F32 = 0, WFQ_F16 = 1, WFQ_BF16 = 2 /* not as a convolution's input */ } wfq_dtype_t;
 
 /* Memory layout of the input x: [N][C][H][W] (default) or [N][H][W][C]. */
 typedef enum { WFQ_NCHW = 0, WFQ_NHWC = 1 } wfq_layout_t;
 
-/* Activation applied by the output transform after the optional bias. */
-typedef enum { WFQ_ACT_NONE = 0, WFQ_ACT_RELU = 1, WFQ_ACT_SILU = 2 } wfq_activation_t;
+/* Activation after the optional bias, in the output transform or in the linear layer (GELU there only). */
+typedef enum { WFQ_ACT_NONE = 0, WFQ_ACT_RELU = 1, WFQ_ACT_SILU = 2, WFQ_ACT_GELU = 3 } wfq_activation_t;
 
 /* Buffers that wfq_debug_get can expose (all device memory). */
 typedef enum {
@@ -362,6 +362,112 @@ wfq_status_t wfq_check_device_status(wfq_plan_t *plan, void *stream, int *where)
 
 /* Release the plan and everything it owns (not the workspace).  NULL is accepted. */
 wfq_status_t wfq_plan_destroy(wfq_plan_t *plan);
+
+/* ---- the operators around the convolutions ------------------------------------------------
+ *
+ * A network whose operators are all quantized group-wise to 8 bits (the paper's W8A8 setting, Section 5, quantizes its
+ * linear layers in the same manner as its convolutions) also has rows of C values: the positions or tokens that its
+ * projections and feed-forward layers work on.  These calls quantize such rows, with the root-mean-square norm in front
+ * of them where asked, and multiply them with quantized weights.
+ *
+ * Quantized rows: codes int8 [rows][Cp], Cp = C rounded up to 32, the codes behind C zero; scales fp32 [G][Rs],
+ * G = ceil(C / group_size) groups of consecutive channels (the last one may be shorter), Rs = rows rounded up to 128,
+ * entries behind `rows` neither written nor used.  group_size: a multiple of 32; 0, or C or more: one group per row.
+ * The quantizer is that of the header comment; in addition a group that holds an infinity or a NaN has the scale NaN and
+ * codes 0, so that what is computed from it is NaN.
+ *
+ * Supported: 1 <= C <= 131072; rows >= 0 (0: nothing is done); leading dimensions (elements from row to row) of at least
+ * the row's width, without alignment beyond the element's.  codes must be 32-byte aligned, scales 16-byte.
+ * Rows with 16-byte aligned starts and a C that is a multiple of 8 are read and written in wider pieces; the results are
+ * the same.  All calls are asynchronous, allocate nothing unless stated, and may be captured into a graph.
+ */
+
+/*
+ * h = x + residual, rounded once to `dtype` (without a residual h = x);
+ * u = fl32(h * gain[c]),  rstd = 1 / sqrt(mean(h^2) + eps), sums in fp32 (rows of values whose squares do not fit it,
+ * above about 1e18, are not supported: their scales become 0 or NaN);
+ * codes = the quantizer's codes of u, scales = the quantizer's scales of u times rstd.
+ * The factor rstd is common to a row and cancels in the codes, which therefore do not depend on its rounding.
+ *   x_dev, residual_dev  device, `dtype`, [rows][C] with leading dimensions ldx, ldr; residual_dev may be NULL
+ *   gain_dev             device, fp32 [C]
+ *   h_dev                device, `dtype`, leading dimension ldh, or NULL (always NULL without a residual); may be x_dev
+ *                        or residual_dev itself with the same leading dimension, otherwise it overlaps neither
+ */
+wfq_status_t wfq_rms_norm_quantize(const void *x_dev, long long ldx, const void *residual_dev, long long ldr,
+                                   const float *gain_dev, float eps, wfq_dtype_t dtype, int rows, int C, int group_size,
+                                   void *h_dev, long long ldh, int8_t *codes_dev, float *scales_dev, void *stream);
+
+/* Rows to codes and scales. */
+wfq_status_t wfq_quantize_rows(const void *x_dev, long long ldx, wfq_dtype_t dtype, int rows, int C, int group_size,
+                               int8_t *codes_dev, float *scales_dev, void *stream);
+
+/* The values that codes and scales stand for, code * scale rounded once to `dtype`: v[rows][C], leading dimension ldv. */
+wfq_status_t wfq_dequantize_rows(const int8_t *codes_dev, const float *scales_dev, int rows, int C, int group_size,
+                                 wfq_dtype_t dtype, void *v_dev, long long ldv, void *stream);
+
+/*
+ * Linear layer on int8 operands with one scale per group of channels on both sides:
+ *   z[r][k] = sum_g sx[g][r] sw[g][k] sum_{c in g} xq[r][c] wq[k][c] + bias[k]     (int32 inside a group, fp32 across)
+ *   y[r][k] = act(z[r][k]) + residual[r][k]                                        k < K
+ * or, gated, with weights of 2K rows (K gates, then K values):
+ *   y[r][k] = act(z[r][k]) * z[r][K + k] + residual[r][k]
+ * y is rounded once to the output type.  Which kernel runs, and over how many CTAs the channels of a tile are split,
+ * depends on the number of rows; the fp32 sums over groups are then formed in another order.  The same call gives the
+ * same bits.
+ */
+typedef struct wfq_linear wfq_linear_t; /* opaque, owned by the library */
+
+/* C input channels, K outputs (at most 4194304).  gated: 0 or 1.  Host only. */
+wfq_status_t wfq_linear_create(wfq_linear_t **out, int C, int K, int group_size, int gated);
+
+/* Element type of x in wfq_linear_forward, and of y and the residual (both WFQ_F16 at first).  Host only. */
+wfq_status_t wfq_linear_set_input_dtype(wfq_linear_t *lin, wfq_dtype_t dtype);
+wfq_status_t wfq_linear_set_output_dtype(wfq_linear_t *lin, wfq_dtype_t dtype);
+
+/* bias_dev: device, fp32 [K] ([2K] if gated: gates, then values), caller-owned, or NULL.  Host only. */
+wfq_status_t wfq_linear_set_epilogue(wfq_linear_t *lin, const float *bias_dev, wfq_activation_t act);
+
+/*
+ * Caller-owned device scratch for wfq_linear_forward on up to `rows` rows (codes and scales of x), 1024-byte aligned.
+ * wfq_linear_forward_codes needs none.  The layer belongs to the device that is current in the first of this call,
+ * wfq_linear_prepare_weights and the forward calls, and is refused (WFQ_ERR_INVALID_ARG) on another one.  That call sets
+ * kernel attributes; make it outside any stream capture.
+ */
+size_t wfq_linear_workspace_bytes(const wfq_linear_t *lin, int rows);
+wfq_status_t wfq_linear_set_workspace(wfq_linear_t *lin, void *dev_ptr, size_t bytes, int rows);
+
+/*
+ * Quantizes the weights w[K][C] ([2K][C] if gated), leading dimension ldw, into buffers that the layer owns (allocated
+ * with cudaMalloc by the first call).  Asynchronous on `stream`; may be called again to replace them.
+ */
+wfq_status_t wfq_linear_prepare_weights(wfq_linear_t *lin, const void *w_dev, long long ldw, wfq_dtype_t dtype,
+                                        void *stream);
+
+/*
+ * y = the layer on x[rows][C] (quantized on the way), or on rows that are quantized already with the layer's C and group
+ * size.  residual_dev may be NULL, or y_dev itself with the same leading dimension.  y does not overlap x or the codes.
+ * WFQ_ERR_NOT_PREPARED without weights or workspace, WFQ_ERR_INVALID_ARG for more rows than the workspace is for.  One
+ * layer must not be used from two threads or two streams at the same time.
+ */
+wfq_status_t wfq_linear_forward(wfq_linear_t *lin, const void *x_dev, long long ldx, int rows, const void *residual_dev,
+                                long long ldr, void *y_dev, long long ldy, void *stream);
+wfq_status_t wfq_linear_forward_codes(wfq_linear_t *lin, const int8_t *codes_dev, const float *scales_dev, int rows,
+                                      const void *residual_dev, long long ldr, void *y_dev, long long ldy, void *stream);
+
+/*
+ * Test and profiling switches: WFQ_DEBUG_WAIT_CYCLES, WFQ_DEBUG_SKIP_GEMM_STAGE, and WFQ_DEBUG_GEMM_SHAPE (0: the
+ * library chooses; else 10000 * CTAs per tile (1, 2, 4, 8; at most one per 128 channels) + 1000 * orientation (1: the
+ * accumulator's lanes are rows of x, 2: outputs) + columns per tile (64, 128, 256; orientation 2: 16, 32, 64)).
+ */
+wfq_status_t wfq_linear_set_debug_option(wfq_linear_t *lin, wfq_debug_option_t option, long long value);
+
+/* As wfq_check_device_status; and the weights: WFQ_BUF_WQ int8 [K or 2K][Cp] (gated: gate and value rows alternate),
+ * WFQ_BUF_SW fp32 [G][Kp], Kp = their number rounded up to 256. */
+wfq_status_t wfq_linear_check_status(wfq_linear_t *lin, void *stream, int *where);
+wfq_status_t wfq_linear_debug_get(wfq_linear_t *lin, wfq_buffer_t which, void **dev_ptr, size_t *bytes);
+
+/* Release the layer and what it owns (not the workspace).  NULL is accepted. */
+wfq_status_t wfq_linear_destroy(wfq_linear_t *lin);
 
 /* Static string for a status code. */
 const char *wfq_status_string(wfq_status_t status);

@@ -15,7 +15,7 @@ WFQ_OK, WFQ_ERR_INVALID_ARG, WFQ_ERR_UNSUPPORTED, WFQ_ERR_ALLOC = 0, 1, 2, 3
 WFQ_ERR_NOT_PREPARED, WFQ_ERR_CUDA, WFQ_ERR_TIMEOUT, WFQ_ERR_SCRATCH_TOO_SMALL = 4, 5, 6, 7
 WFQ_STATIC_SCRATCH_FLOATS = 4 * 1024 * 1024
 WFQ_F32, WFQ_F16, WFQ_BF16 = 0, 1, 2
-WFQ_ACT_NONE, WFQ_ACT_RELU, WFQ_ACT_SILU = 0, 1, 2
+WFQ_ACT_NONE, WFQ_ACT_RELU, WFQ_ACT_SILU, WFQ_ACT_GELU = 0, 1, 2, 3
 WFQ_Y_FP32, WFQ_Y_TILE, WFQ_Y_ROW = 0, 1, 2
 WFQ_NCHW, WFQ_NHWC = 0, 1
 WFQ_BUF_XQ, WFQ_BUF_SX, WFQ_BUF_WQ, WFQ_BUF_SW, WFQ_BUF_Y, WFQ_BUF_STATUS = range(6)
@@ -34,6 +34,11 @@ EXPORTS = [
     "wfq_plan_set_epilogue", "wfq_plan_set_full_quant", "wfq_plan_set_output_dtype", "wfq_plan_set_weight_bits",
     "wfq_conv_forward_host_async", "wfq_filters_bytes", "wfq_filters_export", "wfq_filters_import",
     "wfq_plan_set_input_layout",
+    "wfq_rms_norm_quantize", "wfq_quantize_rows", "wfq_dequantize_rows",
+    "wfq_linear_create", "wfq_linear_set_input_dtype", "wfq_linear_set_output_dtype", "wfq_linear_set_epilogue",
+    "wfq_linear_workspace_bytes", "wfq_linear_set_workspace", "wfq_linear_prepare_weights", "wfq_linear_forward",
+    "wfq_linear_forward_codes", "wfq_linear_set_debug_option", "wfq_linear_check_status", "wfq_linear_debug_get",
+    "wfq_linear_destroy",
 ]
 
 _lib = None
@@ -83,6 +88,24 @@ def load():
     lib.wfq_plan_set_input_layout.argtypes = [vp, ci]
     lib.wfq_plan_set_debug_option.argtypes = [vp, ci, ctypes.c_longlong]
     lib.wfq_debug_int8_mma_rate.argtypes = [vp, ci, ci, ctypes.POINTER(ctypes.c_longlong), vp]
+    ll = ctypes.c_longlong
+    lib.wfq_rms_norm_quantize.argtypes = [vp, ll, vp, ll, vp, ctypes.c_float, ci, ci, ci, ci, vp, ll, vp, vp, vp]
+    lib.wfq_quantize_rows.argtypes = [vp, ll, ci, ci, ci, ci, vp, vp, vp]
+    lib.wfq_dequantize_rows.argtypes = [vp, vp, ci, ci, ci, ci, vp, ll, vp]
+    lib.wfq_linear_create.argtypes = [ctypes.POINTER(vp), ci, ci, ci, ci]
+    lib.wfq_linear_set_input_dtype.argtypes = [vp, ci]
+    lib.wfq_linear_set_output_dtype.argtypes = [vp, ci]
+    lib.wfq_linear_set_epilogue.argtypes = [vp, vp, ci]
+    lib.wfq_linear_workspace_bytes.argtypes = [vp, ci]
+    lib.wfq_linear_workspace_bytes.restype = sz
+    lib.wfq_linear_set_workspace.argtypes = [vp, vp, sz, ci]
+    lib.wfq_linear_prepare_weights.argtypes = [vp, vp, ll, ci, vp]
+    lib.wfq_linear_forward.argtypes = [vp, vp, ll, ci, vp, ll, vp, ll, vp]
+    lib.wfq_linear_forward_codes.argtypes = [vp, vp, vp, ci, vp, ll, vp, ll, vp]
+    lib.wfq_linear_set_debug_option.argtypes = [vp, ci, ll]
+    lib.wfq_linear_check_status.argtypes = [vp, vp, ctypes.POINTER(ci)]
+    lib.wfq_linear_debug_get.argtypes = [vp, ci, ctypes.POINTER(vp), ctypes.POINTER(sz)]
+    lib.wfq_linear_destroy.argtypes = [vp]
     lib.wfq_status_string.argtypes = [ci]
     lib.wfq_status_string.restype = ctypes.c_char_p
     lib.wfq_version.restype = ci
@@ -241,6 +264,87 @@ def wfq_plan_destroy(plan):
     _check(load().wfq_plan_destroy(plan), "wfq_plan_destroy")
 
 
+def wfq_rms_norm_quantize(x_dev, ldx, residual_dev, ldr, gain_dev, eps, dtype, rows, C, group_size, h_dev, ldh,
+                          codes_dev, scales_dev, stream=0):
+    status = (_lib or load()).wfq_rms_norm_quantize(x_dev, ldx, residual_dev, ldr, gain_dev, eps, dtype, rows, C,
+                                                    group_size, h_dev, ldh, codes_dev, scales_dev, stream)
+    if status != WFQ_OK:
+        _check(status, "wfq_rms_norm_quantize")
+
+
+def wfq_quantize_rows(x_dev, ldx, dtype, rows, C, group_size, codes_dev, scales_dev, stream=0):
+    _check((_lib or load()).wfq_quantize_rows(x_dev, ldx, dtype, rows, C, group_size, codes_dev, scales_dev, stream),
+           "wfq_quantize_rows")
+
+
+def wfq_dequantize_rows(codes_dev, scales_dev, rows, C, group_size, dtype, v_dev, ldv, stream=0):
+    _check((_lib or load()).wfq_dequantize_rows(codes_dev, scales_dev, rows, C, group_size, dtype, v_dev, ldv, stream),
+           "wfq_dequantize_rows")
+
+
+def wfq_linear_create(C, K, group_size, gated=0):
+    lin = ctypes.c_void_p()
+    _check(load().wfq_linear_create(ctypes.byref(lin), C, K, group_size, int(gated)), "wfq_linear_create")
+    return lin
+
+
+def wfq_linear_set_input_dtype(lin, dtype):
+    _check(load().wfq_linear_set_input_dtype(lin, dtype), "wfq_linear_set_input_dtype")
+
+
+def wfq_linear_set_output_dtype(lin, dtype):
+    _check(load().wfq_linear_set_output_dtype(lin, dtype), "wfq_linear_set_output_dtype")
+
+
+def wfq_linear_set_epilogue(lin, bias_dev, act=WFQ_ACT_NONE):
+    _check(load().wfq_linear_set_epilogue(lin, bias_dev, act), "wfq_linear_set_epilogue")
+
+
+def wfq_linear_workspace_bytes(lin, rows):
+    return int(load().wfq_linear_workspace_bytes(lin, rows))
+
+
+def wfq_linear_set_workspace(lin, dev_ptr, nbytes, rows):
+    _check(load().wfq_linear_set_workspace(lin, dev_ptr, nbytes, rows), "wfq_linear_set_workspace")
+
+
+def wfq_linear_prepare_weights(lin, w_dev, ldw, dtype, stream=0):
+    _check(load().wfq_linear_prepare_weights(lin, w_dev, ldw, dtype, stream), "wfq_linear_prepare_weights")
+
+
+def wfq_linear_forward(lin, x_dev, ldx, rows, residual_dev, ldr, y_dev, ldy, stream=0):
+    status = (_lib or load()).wfq_linear_forward(lin, x_dev, ldx, rows, residual_dev, ldr, y_dev, ldy, stream)
+    if status != WFQ_OK:
+        _check(status, "wfq_linear_forward")
+
+
+def wfq_linear_forward_codes(lin, codes_dev, scales_dev, rows, residual_dev, ldr, y_dev, ldy, stream=0):
+    status = (_lib or load()).wfq_linear_forward_codes(lin, codes_dev, scales_dev, rows, residual_dev, ldr, y_dev, ldy,
+                                                       stream)
+    if status != WFQ_OK:
+        _check(status, "wfq_linear_forward_codes")
+
+
+def wfq_linear_set_debug_option(lin, option, value):
+    _check(load().wfq_linear_set_debug_option(lin, option, value), "wfq_linear_set_debug_option")
+
+
+def wfq_linear_check_status(lin, stream=0):
+    where = ctypes.c_int(0)
+    st = load().wfq_linear_check_status(lin, stream, ctypes.byref(where))
+    return st, where.value
+
+
+def wfq_linear_debug_get(lin, which):
+    ptr, nbytes = ctypes.c_void_p(), ctypes.c_size_t()
+    _check(load().wfq_linear_debug_get(lin, which, ctypes.byref(ptr), ctypes.byref(nbytes)), "wfq_linear_debug_get")
+    return ptr.value, nbytes.value
+
+
+def wfq_linear_destroy(lin):
+    _check(load().wfq_linear_destroy(lin), "wfq_linear_destroy")
+
+
 # ---- convenience wrapper holding torch tensors for the device buffers ----------------
 
 class _DevicePointer:
@@ -382,6 +486,211 @@ class Conv:
         if self.plan is not None:
             wfq_plan_destroy(self.plan)
             self.plan = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ---- the operators around the convolutions --------------------------------------------
+
+_DTYPES = {"f32": WFQ_F32, "f16": WFQ_F16, "bf16": WFQ_BF16}
+
+
+def _torch_dtypes():
+    import torch
+    return {torch.float32: WFQ_F32, torch.float16: WFQ_F16, torch.bfloat16: WFQ_BF16}
+
+
+def _rows_of(x, C, what):
+    """Rows and leading dimension of a tensor [..., C] whose rows lie one after another at one distance."""
+    assert x.is_cuda and x.dim() >= 1 and x.shape[-1] == C, what
+    rows = x.numel() // C
+    if x.is_contiguous() or rows == 0:
+        return rows, C
+    assert C == 1 or x.stride(-1) == 1, f"{what}: channels must be contiguous"
+    ld, span = None, 1                   # distance between rows, rows that the dimensions behind this one hold
+    for size, stride in zip(reversed(x.shape[:-1]), reversed(x.stride()[:-1])):
+        if size != 1:
+            if ld is None:
+                ld = stride
+            assert stride == ld * span, f"{what}: rows must lie at one distance from each other"
+        span *= size
+    ld = C if ld is None else ld
+    assert rows == 1 or ld >= C, f"{what}: rows overlap"
+    return rows, max(ld, C)
+
+
+class QuantizedRows:
+    """int8 codes [rows][Cp] and fp32 scales [G][Rs] of rows of C channels (layouts: include/wfq.h)."""
+
+    def __init__(self, rows, C, group_size, device, shape=None):
+        import torch
+        self.rows, self.C, self.group_size = rows, C, group_size
+        self.shape = tuple(shape) if shape is not None else (rows, C)
+        groups = 1 if group_size == 0 or group_size >= C else -(-C // group_size)
+        self.codes = torch.empty((rows, (C + 31) // 32 * 32), dtype=torch.int8, device=device)
+        self.scales = torch.empty((groups, (rows + 127) // 128 * 128), dtype=torch.float32, device=device)
+
+
+class _on:
+    """The device of a tensor made current for a call, where it is not already; gives the current raw stream."""
+    __slots__ = ("guard", "index")
+
+    def __init__(self, device):
+        self.index = device.index
+
+    def __enter__(self):
+        import torch
+        here = torch._C._cuda_getDevice()
+        self.guard = None
+        if self.index is not None and self.index != here:
+            self.guard = torch.cuda.device(self.index)
+            self.guard.__enter__()
+            here = self.index
+        return torch._C._cuda_getCurrentRawStream(here)
+
+    def __exit__(self, *args):
+        if self.guard is not None:
+            self.guard.__exit__(*args)
+
+
+def rms_norm_quantize(x, gain, eps=1e-6, group_size=128, residual=None, out=None):
+    """Root-mean-square norm of the rows of x (+ residual) as (QuantizedRows, h).
+
+    x, residual: CUDA tensors [..., C] of one type (fp32, fp16, bf16); gain: fp32 [C].  h is the sum in x's type, written
+    to `out` where given (residual itself is allowed); without a residual it is x."""
+    import torch
+    C = gain.numel()
+    dtypes = _torch_dtypes()
+    assert x.dtype in dtypes, "x: fp32, fp16 or bf16"
+    assert gain.is_cuda and gain.device == x.device and gain.dtype == torch.float32 and gain.is_contiguous()
+    rows, ldx = _rows_of(x, C, "x")
+    q = QuantizedRows(rows, C, group_size, x.device, x.shape)
+    h, ldr, ldh = None, 0, 0
+    if residual is not None:
+        assert residual.shape == x.shape and residual.dtype == x.dtype and residual.device == x.device
+        _, ldr = _rows_of(residual, C, "residual")
+        h = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        assert h.shape == x.shape and h.dtype == x.dtype and h.device == x.device
+        _, ldh = _rows_of(h, C, "out")
+    else:
+        assert out is None, "out: only with a residual"
+    with _on(x.device) as stream:
+        wfq_rms_norm_quantize(x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr, gain.data_ptr(),
+                              eps, dtypes[x.dtype], rows, C, group_size, None if h is None else h.data_ptr(), ldh,
+                              q.codes.data_ptr(), q.scales.data_ptr(), stream)
+    return q, x if h is None else h
+
+
+def quantize_rows(x, group_size=128):
+    """The rows of a CUDA tensor [..., C] as QuantizedRows."""
+    dtypes = _torch_dtypes()
+    assert x.dtype in dtypes, "x: fp32, fp16 or bf16"
+    C = x.shape[-1]
+    rows, ldx = _rows_of(x, C, "x")
+    q = QuantizedRows(rows, C, group_size, x.device, x.shape)
+    with _on(x.device) as stream:
+        wfq_quantize_rows(x.data_ptr(), ldx, dtypes[x.dtype], rows, C, group_size, q.codes.data_ptr(),
+                          q.scales.data_ptr(), stream)
+    return q
+
+
+def dequantize_rows(q, dtype="f16"):
+    """The values of QuantizedRows in "f32", "f16" or "bf16", shaped like the tensor they came from."""
+    import torch
+    v = torch.empty(q.shape, dtype={"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[dtype],
+                    device=q.codes.device)
+    with _on(v.device) as stream:
+        wfq_dequantize_rows(q.codes.data_ptr(), q.scales.data_ptr(), q.rows, q.C, q.group_size, _DTYPES[dtype],
+                            v.data_ptr(), q.C, stream)
+    return v
+
+
+class Linear:
+    """A linear layer on group-wise int8 operands (include/wfq.h): C channels to K outputs, up to max_rows rows a call."""
+
+    def __init__(self, C, K, group_size=128, max_rows=1, dtype="f16", out_dtype=None, gated=False, device="cuda:0"):
+        import torch
+        self.torch = torch
+        self.C, self.K, self.gs, self.gated = C, K, group_size, bool(gated)
+        self.max_rows = max_rows
+        self.device = torch.device(device)
+        names = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+        self._in, self._out = names[dtype], names[out_dtype or dtype]
+        self._bias = None
+        self.lin = None
+        self.lin = wfq_linear_create(C, K, group_size, gated)
+        wfq_linear_set_input_dtype(self.lin, _DTYPES[dtype])
+        wfq_linear_set_output_dtype(self.lin, _DTYPES[out_dtype or dtype])
+        nbytes = wfq_linear_workspace_bytes(self.lin, max_rows)
+        self._ws = torch.empty(nbytes + 1024, dtype=torch.uint8, device=self.device)
+        self.device = self._ws.device
+        with _on(self.device):
+            wfq_linear_set_workspace(self.lin, (self._ws.data_ptr() + 1023) // 1024 * 1024, nbytes, max_rows)
+
+    def prepare(self, w):
+        """w: CUDA tensor [K][C] ([2K][C] if gated: gates, then values), fp32, fp16 or bf16."""
+        dtypes = _torch_dtypes()
+        assert w.device == self.device and w.dtype in dtypes
+        assert w.shape == ((2 if self.gated else 1) * self.K, self.C)
+        _, ldw = _rows_of(w, self.C, "w")
+        with _on(self.device) as stream:
+            wfq_linear_prepare_weights(self.lin, w.data_ptr(), ldw, dtypes[w.dtype], stream)
+
+    def set_epilogue(self, bias=None, act=WFQ_ACT_NONE):
+        """bias: fp32 CUDA tensor [K] ([2K] if gated) or None; kept alive by this object."""
+        if bias is not None:
+            assert bias.device == self.device and bias.dtype == self.torch.float32 and bias.is_contiguous()
+            assert bias.numel() == (2 if self.gated else 1) * self.K
+        wfq_linear_set_epilogue(self.lin, None if bias is None else bias.data_ptr(), act)
+        self._bias = bias
+
+    def _outputs(self, lead, rows, residual, y):
+        shape = (*lead, self.K)
+        if y is None:
+            y = self.torch.empty(shape, dtype=self._out, device=self.device)
+            ldy = self.K
+        else:
+            assert y.shape == shape and y.dtype is self._out and y.device == self.device
+            _, ldy = _rows_of(y, self.K, "y")
+        ldr = 0
+        if residual is not None:
+            assert residual.shape == shape and residual.dtype is self._out and residual.device == self.device
+            _, ldr = _rows_of(residual, self.K, "residual")
+        return y, ldy, None if residual is None else residual.data_ptr(), ldr
+
+    def forward(self, x, residual=None, y=None):
+        """x [..., C] -> y [..., K] (+ residual, which may be y)."""
+        assert x.dtype is self._in and x.device == self.device
+        rows, ldx = _rows_of(x, self.C, "x")
+        y, ldy, res, ldr = self._outputs(x.shape[:-1], rows, residual, y)
+        with _on(self.device) as stream:
+            wfq_linear_forward(self.lin, x.data_ptr(), ldx, rows, res, ldr, y.data_ptr(), ldy, stream)
+        return y
+
+    def forward_codes(self, q, residual=None, y=None):
+        """The same on QuantizedRows of C channels in this layer's groups."""
+        assert q.C == self.C and q.codes.device == self.device
+        assert q.group_size == self.gs or (len(q.scales) == 1 and (self.gs == 0 or self.gs >= self.C))
+        y, ldy, res, ldr = self._outputs(q.shape[:-1], q.rows, residual, y)
+        with _on(self.device) as stream:
+            wfq_linear_forward_codes(self.lin, q.codes.data_ptr(), q.scales.data_ptr(), q.rows, res, ldr, y.data_ptr(),
+                                     ldy, stream)
+        return y
+
+    def check_status(self):
+        with _on(self.device) as stream:
+            st, where = wfq_linear_check_status(self.lin, stream)
+        if st != WFQ_OK:
+            raise WfqError(st, f"device status (wait id {where})")
+
+    def close(self):
+        if self.lin is not None:
+            wfq_linear_destroy(self.lin)
+            self.lin = None
 
     def __del__(self):
         try:

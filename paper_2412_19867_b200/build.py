@@ -9,9 +9,10 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libwfq.so")
 SOURCES = ["wfq_api.cu", "wfq_filter_prep.cu", "wfq_input_transform.cu", "wfq_input_transform_tc.cu",
-           "wfq_input_transform_tcn.cu", "wfq_gemm.cu", "wfq_output_transform.cu", "wfq_full_quant.cu"]
+           "wfq_input_transform_tcn.cu", "wfq_gemm.cu", "wfq_output_transform.cu", "wfq_full_quant.cu",
+           "wfq_rows.cu", "wfq_linear.cu"]
 HEADERS = ["wfq_internal.h", "wfq_ptx.cuh", "wfq_quant.cuh", "wfq_int_quant.cuh", "wfq_strip.cuh",
-           "wfq_output_store.cuh"]
+           "wfq_output_store.cuh", "wfq_rows.h"]
 
 
 def _nvcc():

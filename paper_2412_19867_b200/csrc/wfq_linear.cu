@@ -1,0 +1,843 @@
+// Linear layer on group-wise int8 operands:
+//   z[r][k] = sum_g sx[g][r] sw[g][k] (sum_{c in g} xq[r][c] wq[k][c]) + bias[k]
+//   y[r][k] = act(z[r][k]) + residual[r][k],   gated: y[r][j] = act(z[r][j]) z[r][K + j] + residual[r][j]
+//
+// linear_mma_kernel: persistent, warp-specialised, one CTA per SM.  A tile is 128 rows x BN columns of z; "rows" are the
+// 128 TMEM lanes of the accumulator: rows of x, or with SWAP output channels (few rows of x, so that all lanes carry
+// work).  Gated weights are stored with gate and value channels alternating, so that a pair is two neighbours.
+//   warp 0      TMA producer: 128 channels of both operands per stage (128-byte swizzle)
+//   warp 1      allocates TMEM, issues tcgen05.mma kind::i8 (K = 32): a piece is the part of a group that this CTA has;
+//               pieces of a chunk (up to 128 channels where the group divides 128) lie side by side in one TMEM slot
+//   warp 2      scale loader: 128 row scales and BN column scales per piece
+//   warps 4-11  epilogue: int32 sums to fp32, times the scales, into registers; then bias, activation, gate, residual
+// With few tiles a cluster of up to eight CTAs shares one: each takes a range of the channels, the partial sums are
+// added in rank order through distributed shared memory, each CTA for a share of the columns.
+// Every wait is bounded; on expiry the CTA records where, stops, drains and frees TMEM.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <new>
+
+#include "wfq_output_store.cuh"
+#include "wfq_ptx.cuh"
+#include "wfq_rows.h"
+
+struct wfq_linear {
+    int C = 0, K = 0, gs = 0, gated = 0;
+    int Cp = 0, G = 0, Kz = 0, Kp = 0;         // Kz: columns of z (2K if gated); Kp: Kz rounded up to 256
+    wfq_dtype_t in_dtype = WFQ_F16, out_dtype = WFQ_F16;
+    const float *bias = nullptr;
+    int act = 0;
+    int device = -1, sm_count = 0;
+    int8_t *Wq = nullptr;                      // [Kz][Cp]
+    float *sW = nullptr;                       // [G][Kp], zero behind Kz
+    int *status = nullptr;                     // int32[4]
+    bool prepared = false;
+    bool fresh = false;                        // weights were written since the last launch that waited for them
+    int8_t *xq = nullptr;                      // workspace: codes of up to max_rows rows
+    float *sx = nullptr;
+    int max_rows = 0;
+    long long wait_cycles = 2000000000LL;
+    int debug_skip_stage = -1;
+    int debug_shape = 0;
+};
+
+namespace wfq {
+
+namespace {
+
+constexpr int BM = 128;
+constexpr int BK = 128;
+constexpr int UK = 32;
+constexpr int NSLOT = 2;
+constexpr int SLOT_COLS = 256;
+constexpr int TMEM_COLS = NSLOT * SLOT_COLS;
+constexpr int A_BYTES = BM * BK;
+constexpr int EPI_WARPS = 8;
+constexpr int FIRST_EPI_WARP = 4;
+constexpr int THREADS = 32 * (FIRST_EPI_WARP + EPI_WARPS);
+constexpr int PATCH_PITCH = 17;                                  // floats; 32 x 16 values of an epilogue warp on their way out
+constexpr int PATCH_FLOATS = 32 * PATCH_PITCH;
+
+struct Shared {
+    uint64_t full[16], empty[16];
+    uint64_t acc_full[NSLOT], slot_free[NSLOT];
+    uint64_t mma_done;
+    uint32_t tmem_base;
+    volatile int abort;
+};
+
+template <int BN>
+struct Cfg {
+    static constexpr int STAGES = BN == 256 ? 4 : BN == 128 ? 6 : BN == 64 ? 8 : 10;
+    static constexpr int B_BYTES = BN * BK;
+    static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
+    static constexpr int CG_MAX = SLOT_COLS / BN < 4 ? SLOT_COLS / BN : 4;      // pieces per chunk at most
+    static constexpr int GROUP_SCALE_FLOATS = BM + BN;
+    static constexpr int SLOT_SCALE_FLOATS = CG_MAX * GROUP_SCALE_FLOATS;
+    static constexpr size_t SMEM_BYTES = 1024 + (size_t)STAGES * STAGE_BYTES + EPI_WARPS * PATCH_FLOATS * 4 +
+                                         (size_t)NSLOT * SLOT_SCALE_FLOATS * 4 + sizeof(Shared);
+    static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
+    static_assert((size_t)BN * (BM + 1) * 4 <= (size_t)STAGES * STAGE_BYTES, "partial sums fit the stages");
+};
+
+struct OutArgs {
+    const float *bias;
+    const void *residual;
+    void *y;
+    long long ldr, ldy;
+    int K, Kz;                 // columns of y and of z
+    int R;                     // rows of x
+    int act, gated, dtype;     // dtype: wfq_dtype_t of residual and y
+};
+
+struct MmaArgs {
+    const float *row_scale, *col_scale;
+    long long row_pitch, col_pitch;
+    int rows, cols;            // (R, Kz), with SWAP (Kz, R)
+    int tiles, MT;             // tiles, blocks of 128 rows
+    int split;                 // CTAs per tile (cluster size)
+    int steps, gsteps, cg;     // MMA steps of 32 channels in all, per group; pieces per chunk
+    int *status;
+    long long wait_cycles;
+    int debug_skip_stage;
+    int early;                 // the weights may be read before the previous kernel has completed
+    OutArgs out;
+};
+
+// The channels of this CTA: stages, steps and the pieces (parts of groups) that they fall into.
+struct Range { int kb0, kb1, s0, s1, g0, np; };
+__device__ __forceinline__ Range range_of(const MmaArgs &a, int rank)
+{
+    Range r;
+    const int KB = (a.steps + 3) / 4;
+    r.kb0 = (int)((long long)KB * rank / a.split);
+    r.kb1 = (int)((long long)KB * (rank + 1) / a.split);
+    r.s0 = 4 * r.kb0;
+    r.s1 = min(a.steps, 4 * r.kb1);
+    r.g0 = r.s0 / a.gsteps;
+    r.np = (r.s1 - 1) / a.gsteps - r.g0 + 1;
+    return r;
+}
+
+__device__ __forceinline__ float gelu(float t) { return 0.5f * t * (1.f + erff(t * 0.70710678118654752f)); }
+__device__ __forceinline__ float activate(float t, int act)
+{
+    switch (act) {
+        case WFQ_ACT_RELU: return fmaxf(t, 0.f);
+        case WFQ_ACT_SILU: return silu(t);
+        case WFQ_ACT_GELU: return gelu(t);
+        default: return t;
+    }
+}
+
+__device__ __forceinline__ float out_load(const void *p, long long i, int dtype)
+{
+    if (dtype == WFQ_F32) return static_cast<const float *>(p)[i];
+    if (dtype == WFQ_F16) return __half2float(static_cast<const __half *>(p)[i]);
+    return __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
+}
+__device__ __forceinline__ void out_store(void *p, long long i, float v, int dtype)
+{
+    if (dtype == WFQ_F32) static_cast<float *>(p)[i] = v;
+    else if (dtype == WFQ_F16) static_cast<__half *>(p)[i] = __float2half_rn(v);
+    else static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
+}
+
+// Columns k and k + 1 (k even) of row r of z.
+__device__ __forceinline__ void finish_pair(const OutArgs &o, int r, int k, float v0, float v1)
+{
+    if (r >= o.R || k >= o.Kz) return;
+    if (o.gated) {
+        const int j = k >> 1;
+        if (o.bias) { v0 += __ldg(o.bias + j); v1 += __ldg(o.bias + o.K + j); }
+        float y = activate(v0, o.act) * v1;
+        if (o.residual) y += out_load(o.residual, r * o.ldr + j, o.dtype);
+        out_store(o.y, r * o.ldy + j, y, o.dtype);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        float y = i ? v1 : v0;
+        if (k + i >= o.Kz) return;
+        if (o.bias) y += __ldg(o.bias + k + i);
+        y = activate(y, o.act);
+        if (o.residual) y += out_load(o.residual, r * o.ldr + k + i, o.dtype);
+        out_store(o.y, r * o.ldy + k + i, y, o.dtype);
+    }
+}
+
+// 32 lanes x 16 columns of a tile, as an epilogue warp has them in its patch of shared memory ([lane][column]): from
+// row `row0`, column `col0` of the tile space.
+template <bool SWAP>
+__device__ __noinline__ void finish_patch(const OutArgs &o, const float *patch, int row0, int col0, int ncols)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll 2
+    for (int i = lane; i < 16 * ncols; i += 32) {
+        if constexpr (SWAP) {          // tile rows are columns of z: pairs along the lanes
+            const int p = i & 15, t = i >> 4;
+            finish_pair(o, col0 + t, row0 + 2 * p, patch[2 * p * PATCH_PITCH + t], patch[(2 * p + 1) * PATCH_PITCH + t]);
+        } else {
+            const int half = ncols / 2, p = i % half, t = i / half;
+            finish_pair(o, row0 + t, col0 + 2 * p, patch[t * PATCH_PITCH + 2 * p], patch[t * PATCH_PITCH + 2 * p + 1]);
+        }
+    }
+}
+
+template <int BN, bool SWAP>
+__device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, const WaitCtx &ctx, uint32_t tmem,
+                                              const float *scales, float *patch, float *partial, int half, int quarter,
+                                              int lane, int row0, int col0, const Range &rg, int &slot, uint32_t &sphase)
+{
+    using C = Cfg<BN>;
+    constexpr int CW = BN / 2;                    // columns of a warp
+    constexpr int LD = CW < 16 ? CW : 16;         // columns of one tensor-memory load
+    const int c0 = half * CW;
+    const bool active = row0 + quarter * 32 < a.rows && col0 + c0 < a.cols;
+    float2 acc[CW / 2];
+#pragma unroll
+    for (int j = 0; j < CW / 2; ++j) acc[j] = make_float2(0.f, 0.f);
+    for (int q0 = 0; q0 < rg.np; q0 += a.cg) {
+        const int n = min(a.cg, rg.np - q0);
+        if (!wait_warp(ptx::smem_u32(&sh->acc_full[slot]), sphase, ctx, kWaitTmemFull)) return false;
+        if (active) {
+            ptx::tc_fence_after();
+            const float *sc = scales + (size_t)slot * C::SLOT_SCALE_FLOATS;
+            for (int j = 0; j < n; ++j) {
+                const uint32_t taddr = tmem + (uint32_t)(slot * SLOT_COLS + j * BN + c0);
+                const float rs = sc[j * C::GROUP_SCALE_FLOATS + quarter * 32 + lane];
+                const float2 rs2 = make_float2(rs, rs);
+                const float *cs = sc + j * C::GROUP_SCALE_FLOATS + BM + c0;
+#pragma unroll
+                for (int h = 0; h < CW / LD; ++h) {
+                    uint32_t r[LD];
+                    if constexpr (LD == 16) ptx::tmem_ld_x16(taddr + (uint32_t)(LD * h), r);
+                    else ptx::tmem_ld_x8(taddr + (uint32_t)(LD * h), r);
+                    ptx::tmem_ld_wait(r);
+#pragma unroll
+                    for (int i = 0; i < LD; i += 2) {
+                        const float2 c2 = *reinterpret_cast<const float2 *>(cs + LD * h + i);
+                        const float2 f = make_float2(__int2float_rn((int)r[i]), __int2float_rn((int)r[i + 1]));
+                        acc[(LD * h + i) / 2] = __ffma2_rn(__fmul2_rn(f, rs2), c2, acc[(LD * h + i) / 2]);
+                    }
+                }
+            }
+            ptx::tc_fence_before();
+        }
+        __syncwarp();
+        if (ptx::elect_one()) ptx::mbar_arrive(ptx::smem_u32(&sh->slot_free[slot]));
+        if (++slot == NSLOT) { slot = 0; sphase ^= 1u; }
+    }
+    if (a.split > 1) {           // [column][lane of TMEM], one float of padding per column
+#pragma unroll
+        for (int j = 0; j < CW; ++j)
+            partial[(c0 + j) * (BM + 1) + quarter * 32 + lane] = j & 1 ? acc[j / 2].y : acc[j / 2].x;
+        return true;
+    }
+    if (active) {
+#pragma unroll
+        for (int h = 0; h < CW; h += LD) {
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < LD; ++i)
+                patch[lane * PATCH_PITCH + i] = (h + i) & 1 ? acc[(h + i) / 2].y : acc[(h + i) / 2].x;
+            __syncwarp();
+            finish_patch<SWAP>(a.out, patch, row0 + quarter * 32, col0 + c0 + h, LD);
+        }
+        __syncwarp();
+    }
+    return true;
+}
+
+template <int BN, bool SWAP>
+__global__ void __launch_bounds__(THREADS, 1)
+linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, MmaArgs a)
+{
+    using C = Cfg<BN>;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *tiles = ptx::align_smem<1024>(smem_raw);
+    float *patches = reinterpret_cast<float *>(tiles + (size_t)C::STAGES * C::STAGE_BYTES);
+    float *scales = patches + EPI_WARPS * PATCH_FLOATS;
+    Shared *sh = reinterpret_cast<Shared *>(scales + (size_t)NSLOT * C::SLOT_SCALE_FLOATS);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)blockIdx.x % a.split, first = (int)blockIdx.x / a.split, stride = (int)gridDim.x / a.split;
+    const Range rg = range_of(a, rank);
+    const WaitCtx ctx{&sh->abort, a.status, a.wait_cycles};
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::STAGES; ++s) {
+            ptx::mbar_init(ptx::smem_u32(&sh->full[s]), 1);
+            ptx::mbar_init(ptx::smem_u32(&sh->empty[s]), 1);
+        }
+        for (int s = 0; s < NSLOT; ++s) {
+            ptx::mbar_init(ptx::smem_u32(&sh->acc_full[s]), 2);       // MMAs, scales
+            ptx::mbar_init(ptx::smem_u32(&sh->slot_free[s]), EPI_WARPS);
+        }
+        ptx::mbar_init(ptx::smem_u32(&sh->mma_done), 1);
+        sh->abort = 0;
+        ptx::fence_mbar_init();
+    }
+    if (warp == 1) {
+        ptx::tmem_alloc(ptx::smem_u32(&sh->tmem_base), TMEM_COLS);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem_base = sh->tmem_base;
+    if (warp == 0 && ptx::elect_one()) {
+        ptx::prefetch_tmap(&tmA);
+        ptx::prefetch_tmap(&tmB);
+    }
+    if (warp == 0) __syncwarp();
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
+
+    if (warp == 0) {
+        // ---------------- TMA producer ----------------
+        int stage = 0;
+        uint32_t phase = 0;
+        long long issued = 0;
+        bool ok = true;
+        for (int t = first; t < a.tiles && ok; t += stride) {
+            const int mt = t % a.MT, nt = t / a.MT;
+            for (int kb = rg.kb0; kb < rg.kb1; ++kb) {
+                ok = wait_warp(ptx::smem_u32(&sh->empty[stage]), phase ^ 1u, ctx, kWaitSmemEmpty);
+                if (!ok) break;
+                if (ptx::elect_one() && !(blockIdx.x == 0 && issued == a.debug_skip_stage)) {
+                    const uint32_t bar = ptx::smem_u32(&sh->full[stage]);
+                    const uint32_t dst = ptx::smem_u32(tiles + (size_t)stage * C::STAGE_BYTES);
+                    ptx::mbar_arrive_expect_tx(bar, C::STAGE_BYTES);
+                    ptx::tma_load_2d(dst, &tmA, bar, kb * BK, mt * BM);
+                    ptx::tma_load_2d(dst + A_BYTES, &tmB, bar, kb * BK, nt * BN);
+                }
+                __syncwarp();
+                ++issued;
+                if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+            }
+        }
+        if (!ok || sh->abort) {      // give copies in flight a bounded time to land
+            int s = stage;
+            uint32_t ph = phase;
+            const long long n = issued < C::STAGES ? issued : C::STAGES;
+            for (long long i = 0; i < n; ++i) {
+                if (--s < 0) { s = C::STAGES - 1; ph ^= 1u; }
+                drain(ptx::smem_u32(&sh->full[s]), ph);
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------- MMA issuer ----------------
+        constexpr uint32_t dhi = ptx::smem_desc_sw128_hi();
+        constexpr uint32_t idesc = ptx::idesc_i8(BM, BN);
+        const uint32_t tiles_lo = ptx::smem_desc_sw128_lo(ptx::smem_u32(tiles));
+        int stage = 0, slot = 0;
+        uint32_t phase = 0, sphase = 0;
+        bool ok = true;
+        for (int t = first; t < a.tiles && ok; t += stride) {
+            int in_chunk = 0;                       // pieces of the current chunk that are complete
+            int in_group = rg.s0 % a.gsteps;        // steps into the current group
+            bool fresh = true;                      // the next step is the first of its piece
+            uint32_t dcol = 0;
+            for (int kb = rg.kb0; kb < rg.kb1 && ok; ++kb) {
+                ok = wait_warp(ptx::smem_u32(&sh->full[stage]), phase, ctx, kWaitSmemFull);
+                if (!ok) break;
+                ptx::tc_fence_after();
+                const uint32_t a_lo = tiles_lo + (uint32_t)(stage * (C::STAGE_BYTES >> 4));
+                const uint32_t b_lo = a_lo + (uint32_t)(A_BYTES >> 4);
+                const int n = min(4, rg.s1 - 4 * kb);
+                for (int s = 0; s < n; ++s) {
+                    if (fresh && in_chunk == 0) {
+                        ok = wait_warp(ptx::smem_u32(&sh->slot_free[slot]), sphase ^ 1u, ctx, kWaitTmemEmpty);
+                        if (!ok) break;
+                        ptx::tc_fence_after();
+                        dcol = tmem_base + (uint32_t)(slot * SLOT_COLS);
+                    }
+                    if (ptx::elect_one()) {
+                        if (fresh) ptx::umma_i8_lo<false>(dcol, a_lo + 2 * s, b_lo + 2 * s, dhi, idesc);
+                        else ptx::umma_i8_lo<true>(dcol, a_lo + 2 * s, b_lo + 2 * s, dhi, idesc);
+                    }
+                    __syncwarp();
+                    fresh = false;
+                    if (++in_group == a.gsteps || 4 * kb + s + 1 == rg.s1) {
+                        in_group = 0;
+                        fresh = true;
+                        dcol += BN;
+                        if (++in_chunk == a.cg || 4 * kb + s + 1 == rg.s1) {
+                            if (ptx::elect_one()) ptx::umma_commit(ptx::smem_u32(&sh->acc_full[slot]));
+                            __syncwarp();
+                            in_chunk = 0;
+                            if (++slot == NSLOT) { slot = 0; sphase ^= 1u; }
+                        }
+                    }
+                }
+                if (!ok) break;
+                if (ptx::elect_one()) ptx::umma_commit(ptx::smem_u32(&sh->empty[stage]));
+                __syncwarp();
+                if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+            }
+        }
+    } else if (warp == 2) {
+        // ---------------- scale loader ----------------
+        int slot = 0;
+        uint32_t sphase = 0;
+        long long issued = 0;
+        bool ok = true;
+        for (int t = first; t < a.tiles && ok; t += stride) {
+            const int mt = t % a.MT, nt = t / a.MT;
+            for (int q0 = 0; q0 < rg.np; q0 += a.cg) {
+                const int n = min(a.cg, rg.np - q0);
+                ok = wait_warp(ptx::smem_u32(&sh->slot_free[slot]), sphase ^ 1u, ctx, kWaitScaleEmpty);
+                if (!ok) break;
+                const uint32_t bar = ptx::smem_u32(&sh->acc_full[slot]);
+                const uint32_t dst = ptx::smem_u32(scales + (size_t)slot * C::SLOT_SCALE_FLOATS);
+                if (ptx::elect_one()) ptx::mbar_arrive_expect_tx(bar, (uint32_t)(n * C::GROUP_SCALE_FLOATS * 4));
+                __syncwarp();
+                if (lane < 8 && (lane & 3) < n) {      // lane j: row scales of piece j, lane 4 + j: column scales
+                    const int j = lane & 3;
+                    const long long g = rg.g0 + q0 + j;
+                    const uint32_t d = dst + (uint32_t)(j * C::GROUP_SCALE_FLOATS * 4);
+                    if (lane < 4) ptx::bulk_load(d, a.row_scale + g * a.row_pitch + mt * BM, BM * 4, bar);
+                    else ptx::bulk_load(d + BM * 4, a.col_scale + g * a.col_pitch + nt * BN, BN * 4, bar);
+                }
+                __syncwarp();
+                ++issued;
+                if (++slot == NSLOT) { slot = 0; sphase ^= 1u; }
+            }
+        }
+        if (!ok || sh->abort) {
+            int s = slot;
+            uint32_t ph = sphase;
+            const long long n = issued < NSLOT ? issued : NSLOT;
+            for (long long i = 0; i < n; ++i) {
+                if (--s < 0) { s = NSLOT - 1; ph ^= 1u; }
+                drain(ptx::smem_u32(&sh->acc_full[s]), ph);
+            }
+        }
+    } else if (warp >= FIRST_EPI_WARP) {
+        // ---------------- epilogue ----------------
+        const int e = warp - FIRST_EPI_WARP, quarter = warp & 3;
+        int slot = 0;
+        uint32_t sphase = 0;
+        const uint32_t tmem = tmem_base + ((uint32_t)(quarter * 32) << 16);
+        for (int t = first; t < a.tiles; t += stride) {
+            const int mt = t % a.MT, nt = t / a.MT;
+            if (!epilogue_tile<BN, SWAP>(sh, a, ctx, tmem, scales, patches + e * PATCH_FLOATS,
+                                         reinterpret_cast<float *>(tiles), e >> 2, quarter, lane, mt * BM, nt * BN, rg,
+                                         slot, sphase))
+                break;
+        }
+    }
+
+    __syncwarp();
+    if (a.split > 1) {
+        // one tile per cluster: the partial sums are complete, each CTA adds up its share of the columns in rank order
+        ptx::cluster_sync();
+        const int share = BN / a.split;             // even: at least 2
+        const int mt = first % a.MT, nt = first / a.MT, col0 = rank * share;
+        const uint32_t mine = ptx::smem_u32(tiles);
+        if (first < a.tiles) {
+            for (int i = threadIdx.x; i < BM * share / 2; i += THREADS) {
+                int r0, c0, r1, c1;                 // the pair's places in the tile
+                if constexpr (SWAP) { r0 = 2 * (i % (BM / 2)); r1 = r0 + 1; c0 = c1 = col0 + i / (BM / 2); }
+                else { r0 = r1 = i / (share / 2); c0 = col0 + 2 * (i % (share / 2)); c1 = c0 + 1; }
+                float v0 = 0.f, v1 = 0.f;
+                for (int p = 0; p < a.split; ++p) {
+                    const uint32_t base = ptx::map_rank(mine, (uint32_t)p);
+                    v0 += ptx::ld_cluster(base + (uint32_t)((c0 * (BM + 1) + r0) * 4));
+                    v1 += ptx::ld_cluster(base + (uint32_t)((c1 * (BM + 1) + r1) * 4));
+                }
+                if constexpr (SWAP) finish_pair(a.out, nt * BN + c0, mt * BM + r0, v0, v1);
+                else finish_pair(a.out, mt * BM + r0, nt * BN + c0, v0, v1);
+            }
+        }
+        ptx::cluster_sync();                        // nobody leaves while others read its sums
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        if (sh->abort) {
+            if (ptx::elect_one()) ptx::umma_commit(ptx::smem_u32(&sh->mma_done));
+            __syncwarp();
+            drain(ptx::smem_u32(&sh->mma_done), 0);
+        }
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem_base, TMEM_COLS);
+    }
+}
+
+// How a call is laid out: orientation, columns per tile, CTAs per tile.
+struct Shape { bool swap; int bn, split; };
+
+Shape choose(const wfq_linear &l, int rows)
+{
+    if (l.debug_shape) {
+        const int v = l.debug_shape;
+        return Shape{v / 1000 % 10 == 2, v % 1000, v / 10000};
+    }
+    const int KB = (l.Cp / 32 + 3) / 4;
+    Shape best{false, 64, 1};
+    double best_cost = 1e300;
+    for (int swap = 0; swap < 2; ++swap)
+        for (int bn : {256, 128, 64, 32, 16}) {
+            if (swap ? bn > 64 : bn < 64) continue;
+            const int r = swap ? l.Kz : rows, c = swap ? rows : l.Kz;
+            const double tiles = (double)((r + BM - 1) / BM) * ((c + bn - 1) / bn);
+            for (int split : {1, 2, 4, 8}) {
+                if (split > 1 && (tiles * split > l.sm_count || KB < 2 * split)) continue;
+                const double per_group = BM * bn / 45.0 + 200.0;
+                const double groups = l.gs < 128 ? 128.0 / l.gs : 128.0 / (l.gs < 1024 ? l.gs : 1024);
+                double per_stage = groups * per_group;
+                if (per_stage < (BM + bn) * 128 / 45.0) per_stage = (BM + bn) * 128 / 45.0;
+                const double waves = (double)(long long)((tiles * split + l.sm_count - 1) / l.sm_count);
+                const double cost = waves * (((KB + split - 1) / split) * per_stage + BM * bn / 8.0) +
+                                    (split > 1 ? 2000.0 : 0.0);
+                if (cost < best_cost) { best_cost = cost; best = Shape{swap != 0, bn, split}; }
+            }
+        }
+    return best;
+}
+
+bool encode_codes(CUtensorMap *map, const int8_t *codes, int Cp, int rows, int box_rows)
+{
+    const unsigned long long dims[2] = {(unsigned long long)Cp, (unsigned long long)rows};
+    const unsigned long long strides[1] = {(unsigned long long)Cp};
+    const unsigned box[2] = {128u, (unsigned)box_rows};
+    return encode_tmap(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, codes, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+template <int BN, bool SWAP>
+cudaError_t setup_variant()
+{
+    return cudaFuncSetAttribute(linear_mma_kernel<BN, SWAP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                (int)Cfg<BN>::SMEM_BYTES);
+}
+
+template <int BN, bool SWAP>
+cudaError_t launch_variant(const wfq_linear &l, MmaArgs &a, int grid, const int8_t *xq, int rows, cudaStream_t stream,
+                           bool pdl)
+{
+    a.cg = 1;
+    if (BK % l.gs == 0) a.cg = BK / l.gs < Cfg<BN>::CG_MAX ? BK / l.gs : Cfg<BN>::CG_MAX;
+    CUtensorMap tx, tw;
+    if (!encode_codes(&tx, xq, l.Cp, rows, SWAP ? BN : BM) || !encode_codes(&tw, l.Wq, l.Cp, l.Kz, SWAP ? BM : BN))
+        return cudaErrorInvalidValue;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = Cfg<BN>::SMEM_BYTES;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (pdl) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (a.split > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = (unsigned)a.split;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = (unsigned)n;
+    return cudaLaunchKernelEx(&cfg, linear_mma_kernel<BN, SWAP>, SWAP ? tw : tx, SWAP ? tx : tw, a);
+}
+
+cudaError_t launch_product(wfq_linear &l, const int8_t *xq, const float *sx, int rows, const OutArgs &out,
+                           cudaStream_t stream, bool pdl)
+{
+    const Shape sp = choose(l, rows);
+    MmaArgs a;
+    const long long sx_pitch = (rows + 127LL) / 128 * 128;
+    a.row_scale = sp.swap ? l.sW : sx;
+    a.col_scale = sp.swap ? sx : l.sW;
+    a.row_pitch = sp.swap ? l.Kp : sx_pitch;
+    a.col_pitch = sp.swap ? sx_pitch : l.Kp;
+    a.rows = sp.swap ? l.Kz : rows;
+    a.cols = sp.swap ? rows : l.Kz;
+    a.MT = (a.rows + BM - 1) / BM;
+    a.tiles = a.MT * ((a.cols + sp.bn - 1) / sp.bn);
+    a.split = sp.split;
+    a.steps = l.Cp / UK;
+    a.gsteps = l.gs / UK;
+    a.status = l.status;
+    a.wait_cycles = l.wait_cycles;
+    a.debug_skip_stage = l.debug_skip_stage;
+    a.early = 0;
+    a.out = out;
+    const int grid = sp.split > 1 ? a.tiles * sp.split : a.tiles < l.sm_count ? a.tiles : l.sm_count;
+    if (sp.swap) {
+        if (sp.bn == 16) return launch_variant<16, true>(l, a, grid, xq, rows, stream, pdl);
+        if (sp.bn == 32) return launch_variant<32, true>(l, a, grid, xq, rows, stream, pdl);
+        return launch_variant<64, true>(l, a, grid, xq, rows, stream, pdl);
+    }
+    if (sp.bn == 64) return launch_variant<64, false>(l, a, grid, xq, rows, stream, pdl);
+    if (sp.bn == 128) return launch_variant<128, false>(l, a, grid, xq, rows, stream, pdl);
+    return launch_variant<256, false>(l, a, grid, xq, rows, stream, pdl);
+}
+
+bool known(wfq_dtype_t t) { return t == WFQ_F32 || t == WFQ_F16 || t == WFQ_BF16; }
+size_t elem_bytes(wfq_dtype_t t) { return t == WFQ_F32 ? 4 : 2; }
+bool misaligned(const void *p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
+size_t up1024(size_t v) { return (v + 1023) / 1024 * 1024; }
+wfq_status_t to_status(cudaError_t e)
+{
+    return e == cudaSuccess ? WFQ_OK : e == cudaErrorMemoryAllocation ? WFQ_ERR_ALLOC : WFQ_ERR_CUDA;
+}
+
+// Binds the layer to the current device the first time, refuses another one later.
+wfq_status_t bind(wfq_linear *l)
+{
+    int dev = -1, sms = 0;
+    const wfq_status_t s = current_device(&dev, &sms);
+    if (s != WFQ_OK) return s;
+    if (l->device == dev) return WFQ_OK;
+    if (l->device >= 0) return WFQ_ERR_INVALID_ARG;
+    cudaError_t e = setup_variant<16, true>();
+    if (e == cudaSuccess) e = setup_variant<32, true>();
+    if (e == cudaSuccess) e = setup_variant<64, true>();
+    if (e == cudaSuccess) e = setup_variant<64, false>();
+    if (e == cudaSuccess) e = setup_variant<128, false>();
+    if (e == cudaSuccess) e = setup_variant<256, false>();
+    if (e != cudaSuccess) return WFQ_ERR_CUDA;
+    l->device = dev;
+    l->sm_count = sms;
+    return WFQ_OK;
+}
+
+wfq_status_t check_io(const wfq_linear *l, int rows, const void *residual, long long ldr, const void *y, long long ldy)
+{
+    const size_t e = elem_bytes(l->out_dtype);
+    if (!y || ldy < l->K || misaligned(y, e)) return WFQ_ERR_INVALID_ARG;
+    if (residual && (ldr < l->K || misaligned(residual, e))) return WFQ_ERR_INVALID_ARG;
+    if (rows > 0x7fffff00) return WFQ_ERR_UNSUPPORTED;
+    if (((rows + 127LL) / 128) * ((l->Kz + 63LL) / 64) > 0x7fffffffLL) return WFQ_ERR_UNSUPPORTED;
+    return WFQ_OK;
+}
+
+wfq_status_t product(wfq_linear *l, const int8_t *xq, const float *sx, int rows, const void *residual, long long ldr,
+                     void *y, long long ldy, cudaStream_t st, bool weights_waited_for)
+{
+    // The launch may begin before the previous kernel has ended.  Weights that were written since are waited for by an
+    // ordinary launch; not forgotten under capture, where the launch is only recorded.
+    bool pdl = true;
+    if (l->fresh && !weights_waited_for) {
+        pdl = false;
+        cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+        if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) return WFQ_ERR_CUDA;
+        if (cap == cudaStreamCaptureStatusNone) l->fresh = false;
+    }
+    OutArgs o;
+    o.bias = l->bias; o.residual = residual; o.y = y;
+    o.ldr = ldr; o.ldy = ldy;
+    o.K = l->K; o.Kz = l->Kz; o.R = rows;
+    o.act = l->act; o.gated = l->gated; o.dtype = (int)l->out_dtype;
+    return to_status(launch_product(*l, xq, sx, rows, o, st, pdl));
+}
+
+}  // namespace
+
+}  // namespace wfq
+
+using namespace wfq;
+
+extern "C" {
+
+wfq_status_t wfq_linear_create(wfq_linear_t **out, int C, int K, int group_size, int gated)
+{
+    if (!out) return WFQ_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (C < 1 || K < 1 || group_size < 0 || (gated != 0 && gated != 1)) return WFQ_ERR_INVALID_ARG;
+    if (group_size % 32 != 0 || C > kMaxRowChannels || K > (1 << 22)) return WFQ_ERR_UNSUPPORTED;
+    wfq_linear *l = new (std::nothrow) wfq_linear();
+    if (!l) return WFQ_ERR_ALLOC;
+    l->C = C; l->K = K; l->gated = gated;
+    l->Cp = row_pitch_codes(C);
+    l->G = row_groups(C, group_size);
+    l->gs = l->G == 1 ? l->Cp : group_size;
+    l->Kz = gated ? 2 * K : K;
+    l->Kp = (l->Kz + 255) / 256 * 256;
+    *out = l;
+    return WFQ_OK;
+}
+
+wfq_status_t wfq_linear_set_input_dtype(wfq_linear_t *l, wfq_dtype_t dtype)
+{
+    if (!l || !known(dtype)) return WFQ_ERR_INVALID_ARG;
+    l->in_dtype = dtype;
+    return WFQ_OK;
+}
+
+wfq_status_t wfq_linear_set_output_dtype(wfq_linear_t *l, wfq_dtype_t dtype)
+{
+    if (!l || !known(dtype)) return WFQ_ERR_INVALID_ARG;
+    l->out_dtype = dtype;
+    return WFQ_OK;
+}
+
+wfq_status_t wfq_linear_set_epilogue(wfq_linear_t *l, const float *bias_dev, wfq_activation_t act)
+{
+    if (!l || (act != WFQ_ACT_NONE && act != WFQ_ACT_RELU && act != WFQ_ACT_SILU && act != WFQ_ACT_GELU))
+        return WFQ_ERR_INVALID_ARG;
+    if (misaligned(bias_dev, 4)) return WFQ_ERR_INVALID_ARG;
+    l->bias = bias_dev;
+    l->act = (int)act;
+    return WFQ_OK;
+}
+
+size_t wfq_linear_workspace_bytes(const wfq_linear_t *l, int rows)
+{
+    if (!l || rows < 1 || rows > 0x7fffff00) return 0;
+    return up1024((size_t)rows * l->Cp) + up1024((size_t)l->G * ((rows + 127LL) / 128 * 128) * sizeof(float));
+}
+
+wfq_status_t wfq_linear_set_workspace(wfq_linear_t *l, void *dev_ptr, size_t bytes, int rows)
+{
+    if (!l || !dev_ptr || rows < 1 || rows > 0x7fffff00) return WFQ_ERR_INVALID_ARG;
+    if (bytes < wfq_linear_workspace_bytes(l, rows) || misaligned(dev_ptr, 1024)) return WFQ_ERR_INVALID_ARG;
+    const wfq_status_t s = bind(l);
+    if (s != WFQ_OK) return s;
+    l->xq = static_cast<int8_t *>(dev_ptr);
+    l->sx = reinterpret_cast<float *>(static_cast<char *>(dev_ptr) + up1024((size_t)rows * l->Cp));
+    l->max_rows = rows;
+    return WFQ_OK;
+}
+
+wfq_status_t wfq_linear_prepare_weights(wfq_linear_t *l, const void *w_dev, long long ldw, wfq_dtype_t dtype, void *stream)
+{
+    if (!l || !w_dev || !known(dtype) || ldw < l->C || misaligned(w_dev, elem_bytes(dtype))) return WFQ_ERR_INVALID_ARG;
+    const wfq_status_t s = bind(l);
+    if (s != WFQ_OK) return s;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    cudaError_t e;
+    if (!l->Wq && (e = cudaMalloc(&l->Wq, (size_t)l->Kz * l->Cp)) != cudaSuccess) return to_status(e);
+    if (!l->sW) {
+        const size_t n = (size_t)l->G * l->Kp * sizeof(float);
+        float *p = nullptr;
+        if ((e = cudaMalloc(&p, n)) != cudaSuccess) return to_status(e);
+        if (cudaMemsetAsync(p, 0, n, st) != cudaSuccess) { cudaFree(p); return WFQ_ERR_CUDA; }
+        l->sW = p;
+    }
+    if (!l->status) {
+        int *p = nullptr;
+        if ((e = cudaMalloc(&p, 4 * sizeof(int))) != cudaSuccess) return to_status(e);
+        if (cudaMemsetAsync(p, 0, 4 * sizeof(int), st) != cudaSuccess) { cudaFree(p); return WFQ_ERR_CUDA; }
+        l->status = p;
+    }
+    RowsArgs a;
+    a.x = w_dev; a.ldx = ldw;
+    a.codes = l->Wq; a.scales = l->sW;
+    a.rows = l->Kz; a.C = l->C; a.Cp = l->Cp;
+    a.gs = l->gs; a.G = l->G;
+    a.scale_pitch = l->Kp;
+    a.half = l->gated ? l->K : 0;
+    l->fresh = true;
+    if (launch_rows(a, dtype, st, false) != cudaSuccess) { l->prepared = false; return WFQ_ERR_CUDA; }
+    l->prepared = true;
+    return WFQ_OK;
+}
+
+wfq_status_t wfq_linear_forward_codes(wfq_linear_t *l, const int8_t *codes_dev, const float *scales_dev, int rows,
+                                      const void *residual_dev, long long ldr, void *y_dev, long long ldy, void *stream)
+{
+    if (!l || rows < 0) return WFQ_ERR_INVALID_ARG;
+    if (!l->prepared) return WFQ_ERR_NOT_PREPARED;
+    if (rows == 0) return WFQ_OK;
+    wfq_status_t s = check_io(l, rows, residual_dev, ldr, y_dev, ldy);
+    if (s != WFQ_OK) return s;
+    if (!codes_dev || !scales_dev || misaligned(codes_dev, 32) || misaligned(scales_dev, 16)) return WFQ_ERR_INVALID_ARG;
+    if ((s = bind(l)) != WFQ_OK) return s;
+    return product(l, codes_dev, scales_dev, rows, residual_dev, ldr, y_dev, ldy, reinterpret_cast<cudaStream_t>(stream),
+                   false);
+}
+
+wfq_status_t wfq_linear_forward(wfq_linear_t *l, const void *x_dev, long long ldx, int rows, const void *residual_dev,
+                                long long ldr, void *y_dev, long long ldy, void *stream)
+{
+    if (!l || rows < 0) return WFQ_ERR_INVALID_ARG;
+    if (!l->prepared || !l->xq) return WFQ_ERR_NOT_PREPARED;
+    if (rows == 0) return WFQ_OK;
+    wfq_status_t s = check_io(l, rows, residual_dev, ldr, y_dev, ldy);
+    if (s != WFQ_OK) return s;
+    if (!x_dev || ldx < l->C || misaligned(x_dev, elem_bytes(l->in_dtype)) || rows > l->max_rows)
+        return WFQ_ERR_INVALID_ARG;
+    if ((s = bind(l)) != WFQ_OK) return s;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    RowsArgs a;
+    a.x = x_dev; a.ldx = ldx;
+    a.codes = l->xq; a.scales = l->sx;
+    a.rows = rows; a.C = l->C; a.Cp = l->Cp;
+    a.gs = l->gs; a.G = l->G;
+    a.scale_pitch = (rows + 127LL) / 128 * 128;
+    if (launch_rows(a, l->in_dtype, st, true) != cudaSuccess) return WFQ_ERR_CUDA;
+    // the row quantizer lets the product start only after its own wait for what was in front of it, fresh weights too
+    return product(l, l->xq, l->sx, rows, residual_dev, ldr, y_dev, ldy, st, true);
+}
+
+wfq_status_t wfq_linear_set_debug_option(wfq_linear_t *l, wfq_debug_option_t option, long long value)
+{
+    if (!l) return WFQ_ERR_INVALID_ARG;
+    switch (option) {
+        case WFQ_DEBUG_WAIT_CYCLES:
+            if (value < 1000) return WFQ_ERR_INVALID_ARG;
+            l->wait_cycles = value;
+            return WFQ_OK;
+        case WFQ_DEBUG_SKIP_GEMM_STAGE:
+            if (value < -1 || value > 0x7fffffff) return WFQ_ERR_INVALID_ARG;
+            l->debug_skip_stage = (int)value;
+            return WFQ_OK;
+        case WFQ_DEBUG_GEMM_SHAPE: {
+            const long long bn = value % 1000, orient = value / 1000 % 10, split = value / 10000;
+            const bool normal = orient == 1 && (bn == 64 || bn == 128 || bn == 256);
+            const bool swapped = orient == 2 && (bn == 16 || bn == 32 || bn == 64);
+            const bool parts = split == 1 || split == 2 || split == 4 || split == 8;
+            // every CTA of a tile needs at least 128 channels
+            if (value != 0 && (value < 0 || !parts || !(normal || swapped) || (l->Cp + 127) / 128 < split))
+                return WFQ_ERR_INVALID_ARG;
+            l->debug_shape = (int)value;
+            return WFQ_OK;
+        }
+        default: return WFQ_ERR_INVALID_ARG;
+    }
+}
+
+wfq_status_t wfq_linear_check_status(wfq_linear_t *l, void *stream, int *where)
+{
+    if (!l) return WFQ_ERR_INVALID_ARG;
+    if (!l->status) return WFQ_ERR_NOT_PREPARED;
+    int host[4] = {0, 0, 0, 0};
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (cudaMemcpyAsync(host, l->status, sizeof(host), cudaMemcpyDeviceToHost, st) != cudaSuccess) return WFQ_ERR_CUDA;
+    if (cudaStreamSynchronize(st) != cudaSuccess) return WFQ_ERR_CUDA;
+    if (where) *where = host[1];
+    return host[0] == 0 ? WFQ_OK : WFQ_ERR_TIMEOUT;
+}
+
+wfq_status_t wfq_linear_debug_get(wfq_linear_t *l, wfq_buffer_t which, void **dev_ptr, size_t *bytes)
+{
+    if (!l || !dev_ptr || !bytes) return WFQ_ERR_INVALID_ARG;
+    *dev_ptr = nullptr;
+    *bytes = 0;
+    switch (which) {
+        case WFQ_BUF_WQ:
+            if (!l->prepared) return WFQ_ERR_NOT_PREPARED;
+            *dev_ptr = l->Wq; *bytes = (size_t)l->Kz * l->Cp; return WFQ_OK;
+        case WFQ_BUF_SW:
+            if (!l->prepared) return WFQ_ERR_NOT_PREPARED;
+            *dev_ptr = l->sW; *bytes = (size_t)l->G * l->Kp * sizeof(float); return WFQ_OK;
+        default: return WFQ_ERR_INVALID_ARG;
+    }
+}
+
+wfq_status_t wfq_linear_destroy(wfq_linear_t *l)
+{
+    if (!l) return WFQ_OK;
+    if (l->Wq) cudaFree(l->Wq);
+    if (l->sW) cudaFree(l->sW);
+    if (l->status) cudaFree(l->status);
+    delete l;
+    return WFQ_OK;
+}
+
+}  // extern "C"
