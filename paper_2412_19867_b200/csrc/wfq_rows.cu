@@ -87,7 +87,7 @@ __device__ __forceinline__ float rstd_of(float sum, const RowsArgs &a)
     return __fdiv_rn(1.f, __fsqrt_rn(__fadd_rn(__fdiv_rn(sum, (float)a.C), a.eps)));
 }
 
-// Any row: widths and strides without alignment, any group size.  One CTA per row, two passes over it; the second
+// Rows that registers do not hold.  One CTA per row, two passes over it; the second
 // reads the first one's h where it was stored (h may be x or residual itself).
 template <typename T, bool NORM>
 __global__ void __launch_bounds__(256) rows_any_kernel(RowsArgs a)
@@ -156,16 +156,142 @@ __global__ void __launch_bounds__(256) rows_any_kernel(RowsArgs a)
     }
 }
 
-template <typename T>
+// VEC consecutive elements as fp32 (VEC 8: 16-byte aligned).
+template <int VEC, typename T> __device__ __forceinline__ void load(const T *p, float (&v)[VEC])
+{
+    if constexpr (VEC == 8) load8(p, v);
+    else v[0] = Elem<T>::get(*p);
+}
+template <int VEC, typename T> __device__ __forceinline__ void store(T *p, const float (&v)[VEC])
+{
+    if constexpr (VEC == 8) store8(p, v);
+    else *p = Elem<T>::put(v[0]);
+}
+
+// Rows of up to 32768 channels, held in registers: one pass.  `tpr` threads (whole warps) have a row, thread t the
+// vectors t, t + tpr, ... of VEC elements; a CTA has several short rows.  A group of gs = VEC * lanes channels (lanes a
+// power of two up to 32) lies in neighbouring lanes; other groups are joined in shared memory (`direct` 0).
+template <typename T, bool NORM, bool RES, int VEC, int NV>
+__global__ void __launch_bounds__(1024) rows_kernel(RowsArgs a, int tpr, int lanes, int direct)
+{
+    extern __shared__ int group_max[];        // [rows of the CTA][G] where groups are joined
+    __shared__ float warp_sum[32];
+    const int local = (int)threadIdx.x / tpr, t = (int)threadIdx.x - local * tpr, per_cta = (int)blockDim.x / tpr;
+    const long long row = (long long)blockIdx.x * per_cta + local;
+    const bool live = row < a.rows;
+    const int lane = threadIdx.x & 31;
+    int *gmax = group_max + local * a.G;
+    if (!direct) {
+        for (int g = t; g < a.G; g += tpr) gmax[g] = 0;
+        __syncthreads();
+    }
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
+
+    float u[NV][VEC];
+    float sum = 0.f;
+    const int n = live ? a.C / VEC : 0;       // vectors of the row
+    const T *x = static_cast<const T *>(a.x) + row * a.ldx;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int v = i * tpr + t;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) u[i][e] = 0.f;
+        if (v < n) load<VEC>(x + v * VEC, u[i]);
+    }
+    if constexpr (RES) {
+        const T *r = static_cast<const T *>(a.residual) + row * a.ldr;
+        T *h = static_cast<T *>(a.h) + row * a.ldh;
+        float w[NV][VEC];
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i * tpr + t < n) load<VEC>(r + (i * tpr + t) * VEC, w[i]);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i * tpr + t < n) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) u[i][e] = Elem<T>::get(Elem<T>::put(__fadd_rn(u[i][e], w[i][e])));
+                if (a.h) store<VEC>(h + (i * tpr + t) * VEC, u[i]);
+            }
+    }
+    int amax[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int v = i * tpr + t;
+        if constexpr (NORM) {
+            float gain[VEC];
+            if (v < n) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum = fmaf(u[i][e], u[i][e], sum);
+                load<VEC>(a.gain + v * VEC, gain);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) u[i][e] = __fmul_rn(u[i][e], gain[e]);
+            }
+        }
+        amax[i] = 0;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) amax[i] = max(amax[i], magnitude_bits(u[i][e]));
+        for (int o = 1; o < lanes; o <<= 1) amax[i] = max(amax[i], __shfl_xor_sync(0xffffffffu, amax[i], o));
+        if (!direct && v < n && (lane & (lanes - 1)) == 0) atomicMax(&gmax[v * VEC / a.gs], amax[i]);
+    }
+    float rstd = 1.f;
+    if constexpr (NORM) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (tpr > 32) {
+            if (lane == 0) warp_sum[threadIdx.x >> 5] = sum;
+            __syncthreads();
+            sum = 0.f;
+            for (int w = 0; w < tpr / 32; ++w) sum += warp_sum[local * (tpr / 32) + w];
+        }
+        rstd = rstd_of(sum, a);
+    }
+    if (!direct && !(NORM && tpr > 32)) __syncthreads();
+    if (!live) return;
+    const int to = target_row(a, (int)row);
+    int8_t *codes = a.codes + (size_t)to * a.Cp;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int v = i * tpr + t;
+        if (v >= a.Cp / VEC) break;
+        const int g = v * VEC / a.gs;
+        float scale, inv;
+        scale_of(direct ? amax[i] : gmax[g], scale, inv);
+        if (v * VEC == g * a.gs) a.scales[(size_t)g * a.scale_pitch + to] = NORM ? __fmul_rn(scale, rstd) : scale;
+        uint32_t w[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) w[e] = inv > 0.f ? code_bits(u[i][e], inv) : 0u;
+        if constexpr (VEC == 8) {
+            const uint32_t lo = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
+            const uint32_t hi = __byte_perm(__byte_perm(w[4], w[5], 0x0040), __byte_perm(w[6], w[7], 0x0040), 0x5410);
+            *reinterpret_cast<uint2 *>(codes + v * 8) = make_uint2(lo, hi);
+        } else {
+            codes[v] = (int8_t)w[0];
+        }
+    }
+}
+
+// Codes back to values, VEC of them per thread and step.
+template <typename T, int VEC>
 __global__ void __launch_bounds__(256) dequantize_kernel(const int8_t *codes, const float *scales, int rows, int C, int Cp,
-                                                         int gs, long long scale_pitch, T *v, long long ldv)
+                                                         int gs, long long scale_pitch, T *v, long long ldv, int tpr)
 {
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-    for (long long row = blockIdx.y; row < rows; row += gridDim.y)
-        for (int c = blockIdx.x * 256 + threadIdx.x; c < C; c += gridDim.x * 256) {
+    const int local = (int)threadIdx.x / tpr, per_cta = 256 / tpr;
+    if (local >= per_cta) return;
+    for (long long row = (long long)blockIdx.x * per_cta + local; row < rows; row += (long long)gridDim.x * per_cta)
+        for (int c = ((int)threadIdx.x - local * tpr) * VEC; c < C; c += tpr * VEC) {
             const float s = scales[(size_t)(c / gs) * scale_pitch + row];
-            v[row * ldv + c] = Elem<T>::put((float)codes[row * Cp + c] * s);
+            float out[VEC];
+            if constexpr (VEC == 8) {
+                const uint2 q = *reinterpret_cast<const uint2 *>(codes + row * Cp + c);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) out[e] = (float)(int8_t)((e < 4 ? q.x : q.y) >> (8 * (e & 3))) * s;
+            } else {
+                out[0] = (float)codes[row * Cp + c] * s;
+            }
+            store<VEC>(v + row * ldv + c, out);
         }
 }
 
@@ -185,9 +311,51 @@ cudaError_t launch(K kernel, dim3 grid, int threads, size_t smem, cudaStream_t s
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+// Threads and vectors per thread of a row, for E elements per thread.
+template <typename T, bool NORM, bool RES, int VEC, int NV>
+cudaError_t launch_rows_kernel(const RowsArgs &a, int tpr, cudaStream_t stream, bool pdl)
+{
+    // lanes of the largest power of two of channels that no group's border cuts
+    int lanes = 1;
+    while (lanes < 32 && a.gs % (2 * lanes * VEC) == 0) lanes *= 2;
+    const int direct = a.gs == lanes * VEC;
+    const int per_cta = tpr >= 128 || a.rows < 1024 ? 1 : 128 / tpr;
+    const size_t smem = direct ? 0 : (size_t)per_cta * a.G * sizeof(int);
+    return launch(rows_kernel<T, NORM, RES, VEC, NV>, dim3((unsigned)((a.rows + per_cta - 1) / per_cta)), tpr * per_cta, smem,
+                  stream, pdl, a, tpr, lanes, direct);
+}
+
+template <typename T, int VEC, int NV>
+cudaError_t launch_rows_mode(const RowsArgs &a, int tpr, cudaStream_t stream, bool pdl)
+{
+    if (!a.gain) return launch_rows_kernel<T, false, false, VEC, NV>(a, tpr, stream, pdl);
+    if (!a.residual) return launch_rows_kernel<T, true, false, VEC, NV>(a, tpr, stream, pdl);
+    return launch_rows_kernel<T, true, true, VEC, NV>(a, tpr, stream, pdl);
+}
+
+bool aligned16(const void *p, long long ld, size_t elem)
+{
+    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (size_t)ld * elem % 16 == 0;
+}
+
 template <typename T>
 cudaError_t launch_rows_t(const RowsArgs &a, cudaStream_t stream, bool pdl)
 {
+    const size_t e = sizeof(T);
+    const bool wide = a.C % 8 == 0 && aligned16(a.x, a.ldx, e) && (!a.residual || aligned16(a.residual, a.ldr, e)) &&
+                      (!a.h || aligned16(a.h, a.ldh, e)) && (!a.gain || aligned16(a.gain, 0, 4));
+    // elements per thread: 8 where that takes no more than 1024 threads and there are few rows, else 16 or 32
+    for (int per : {8, 16, 32}) {
+        const int tpr = (a.Cp / per + (a.Cp % per != 0) + 31) / 32 * 32;
+        if (tpr > 1024 || (per == 8 && a.rows > 592)) continue;
+        if (wide)
+            return per == 8 ? launch_rows_mode<T, 8, 1>(a, tpr, stream, pdl)
+                            : per == 16 ? launch_rows_mode<T, 8, 2>(a, tpr, stream, pdl)
+                                        : launch_rows_mode<T, 8, 4>(a, tpr, stream, pdl);
+        return per == 8 ? launch_rows_mode<T, 1, 8>(a, tpr, stream, pdl)
+                        : per == 16 ? launch_rows_mode<T, 1, 16>(a, tpr, stream, pdl)
+                                    : launch_rows_mode<T, 1, 32>(a, tpr, stream, pdl);
+    }
     const int grid = a.rows < (1 << 20) ? a.rows : 1 << 20;
     const size_t smem = (size_t)a.G * sizeof(int);
     return a.gain ? launch(rows_any_kernel<T, true>, dim3((unsigned)grid), 256, smem, stream, pdl, a)
@@ -198,10 +366,14 @@ template <typename T>
 cudaError_t launch_dequantize(const int8_t *codes, const float *scales, int rows, int C, int gs, void *v, long long ldv,
                               cudaStream_t stream)
 {
-    const unsigned gx = (unsigned)((C + 255) / 256), gy = (unsigned)(rows < 65535 ? rows : 65535);
-    const long long pitch = (rows + 127LL) / 128 * 128;
-    return launch(dequantize_kernel<T>, dim3(gx, gy), 256, 0, stream, true, codes, scales, rows, C, row_pitch_codes(C), gs,
-                  pitch, static_cast<T *>(v), ldv);
+    const bool wide = C % 8 == 0 && aligned16(v, ldv, sizeof(T));
+    const int n = wide ? C / 8 : C, tpr = n >= 256 ? 256 : (n + 31) / 32 * 32, per_cta = 256 / tpr;
+    const long long ctas = (rows + (long long)per_cta - 1) / per_cta, pitch = (rows + 127LL) / 128 * 128;
+    const dim3 grid((unsigned)(ctas < (1 << 20) ? ctas : 1 << 20));
+    return wide ? launch(dequantize_kernel<T, 8>, grid, 256, 0, stream, true, codes, scales, rows, C, row_pitch_codes(C), gs,
+                         pitch, static_cast<T *>(v), ldv, tpr)
+                : launch(dequantize_kernel<T, 1>, grid, 256, 0, stream, true, codes, scales, rows, C, row_pitch_codes(C), gs,
+                         pitch, static_cast<T *>(v), ldv, tpr);
 }
 
 bool known(wfq_dtype_t t) { return t == WFQ_F32 || t == WFQ_F16 || t == WFQ_BF16; }
