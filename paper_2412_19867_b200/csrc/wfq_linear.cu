@@ -56,8 +56,6 @@ constexpr int A_BYTES = BM * BK;
 constexpr int EPI_WARPS = 8;
 constexpr int FIRST_EPI_WARP = 4;
 constexpr int THREADS = 32 * (FIRST_EPI_WARP + EPI_WARPS);
-constexpr int PATCH_PITCH = 17;                                  // floats; 32 x 16 values of an epilogue warp on their way out
-constexpr int PATCH_FLOATS = 32 * PATCH_PITCH;
 
 struct Shared {
     uint64_t full[16], empty[16];
@@ -75,7 +73,7 @@ struct Cfg {
     static constexpr int CG_MAX = SLOT_COLS / BN < 4 ? SLOT_COLS / BN : 4;      // pieces per chunk at most
     static constexpr int GROUP_SCALE_FLOATS = BM + BN;
     static constexpr int SLOT_SCALE_FLOATS = CG_MAX * GROUP_SCALE_FLOATS;
-    static constexpr size_t SMEM_BYTES = 1024 + (size_t)STAGES * STAGE_BYTES + EPI_WARPS * PATCH_FLOATS * 4 +
+    static constexpr size_t SMEM_BYTES = 1024 + (size_t)STAGES * STAGE_BYTES +
                                          (size_t)NSLOT * SLOT_SCALE_FLOATS * 4 + sizeof(Shared);
     static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
     static_assert((size_t)BN * (BM + 1) * 4 <= (size_t)STAGES * STAGE_BYTES, "partial sums fit the stages");
@@ -89,6 +87,7 @@ struct OutArgs {
     int K, Kz;                 // columns of y and of z
     int R;                     // rows of x
     int act, gated, dtype;     // dtype: wfq_dtype_t of residual and y
+    int vec;                   // rows of y and the residual start on 16-byte boundaries
 };
 
 struct MmaArgs {
@@ -167,27 +166,167 @@ __device__ __forceinline__ void finish_pair(const OutArgs &o, int r, int k, floa
     }
 }
 
-// 32 lanes x 16 columns of a tile, as an epilogue warp has them in its patch of shared memory ([lane][column]): from
-// row `row0`, column `col0` of the tile space.
-template <bool SWAP>
-__device__ __noinline__ void finish_patch(const OutArgs &o, const float *patch, int row0, int col0, int ncols)
+// Eight values of y or the residual at once (`vec`: 16-byte aligned rows).
+struct Pack8 { uint32_t w[8]; };             // 16-bit types: the first four words
+__device__ __forceinline__ Pack8 load_pack(const void *p, long long i, int dtype)
 {
-    const int lane = threadIdx.x & 31;
-#pragma unroll 2
-    for (int i = lane; i < 16 * ncols; i += 32) {
-        if constexpr (SWAP) {          // tile rows are columns of z: pairs along the lanes
-            const int p = i & 15, t = i >> 4;
-            finish_pair(o, col0 + t, row0 + 2 * p, patch[2 * p * PATCH_PITCH + t], patch[(2 * p + 1) * PATCH_PITCH + t]);
-        } else {
-            const int half = ncols / 2, p = i % half, t = i / half;
-            finish_pair(o, row0 + t, col0 + 2 * p, patch[t * PATCH_PITCH + 2 * p], patch[t * PATCH_PITCH + 2 * p + 1]);
+    Pack8 r;
+    const uint4 *q = reinterpret_cast<const uint4 *>(static_cast<const char *>(p) + i * (dtype == WFQ_F32 ? 4 : 2));
+    const uint4 u = q[0];
+    r.w[0] = u.x; r.w[1] = u.y; r.w[2] = u.z; r.w[3] = u.w;
+    if (dtype == WFQ_F32) {
+        const uint4 v = q[1];
+        r.w[4] = v.x; r.w[5] = v.y; r.w[6] = v.z; r.w[7] = v.w;
+    }
+    return r;
+}
+__device__ __forceinline__ void add_pack(float (&y)[8], const Pack8 &r, int dtype)
+{
+    if (dtype == WFQ_F32) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] += __uint_as_float(r.w[i]);
+    } else if (dtype == WFQ_F16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&r.w[i]));
+            y[2 * i] += f.x; y[2 * i + 1] += f.y;
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            y[2 * i] += __uint_as_float(r.w[i] << 16);
+            y[2 * i + 1] += __uint_as_float(r.w[i] & 0xffff0000u);
+        }
+    }
+}
+__device__ __forceinline__ void store_pack(void *p, long long i, const float (&y)[8], int dtype)
+{
+    uint4 *q = reinterpret_cast<uint4 *>(static_cast<char *>(p) + i * (dtype == WFQ_F32 ? 4 : 2));
+    if (dtype == WFQ_F32) {
+        q[0] = make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
+        q[1] = make_uint4(__float_as_uint(y[4]), __float_as_uint(y[5]), __float_as_uint(y[6]), __float_as_uint(y[7]));
+    } else {
+        const int kind = dtype == WFQ_F16 ? 1 : 2;
+        q[0] = make_uint4(to_bits16x2(y[0], y[1], kind), to_bits16x2(y[2], y[3], kind), to_bits16x2(y[4], y[5], kind),
+                          to_bits16x2(y[6], y[7], kind));
+    }
+}
+
+template <int N>
+__device__ __forceinline__ void activate_all(float (&z)[N], int act)
+{
+    if (act == WFQ_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = fmaxf(z[i], 0.f);
+    } else if (act == WFQ_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = silu(z[i]);
+    } else if (act == WFQ_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = gelu(z[i]);
+    }
+}
+
+// Eight outputs of one row from eight (gated: sixteen) columns of z: column j of y on, all of them inside K.
+__device__ __forceinline__ void finish8(const OutArgs &o, long long r, int j, float (&y)[8], const float (&v)[8], const Pack8 &res)
+{
+    activate_all(y, o.act);
+    if (o.gated) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] *= v[i];
+    }
+    if (o.residual) add_pack(y, res, o.dtype);
+    store_pack(o.y, r * o.ldy + j, y, o.dtype);
+}
+
+// CW columns of z that a thread holds for row r, from column k on.
+template <int CW>
+__device__ __forceinline__ void finish_row(const OutArgs &o, int r, int k, const float2 (&acc)[CW / 2])
+{
+    if (r >= o.R) return;
+    auto at = [&](int i) { return i & 1 ? acc[i / 2].y : acc[i / 2].x; };
+    const int step = o.gated ? 16 : 8;
+    const Pack8 none = {};
+    Pack8 next = o.vec && o.residual && k + step <= o.Kz ? load_pack(o.residual, r * o.ldr + (o.gated ? k / 2 : k), o.dtype)
+                                                         : none;
+#pragma unroll
+    for (int h = 0; h < CW; h += 16) {
+        const int k0 = k + h;
+        if (o.vec && k0 + 16 <= o.Kz) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                if (s == 1 && o.gated) break;
+                const int j = o.gated ? k0 / 2 : k0 + 8 * s;
+                const Pack8 res = next;
+                // the next eight, ahead of this store (y may be the residual, element by element)
+                const int kn = o.gated ? k0 + 16 : k0 + 8 * (s + 1);
+                if (o.residual && kn < k + CW && kn + step <= o.Kz)
+                    next = load_pack(o.residual, r * o.ldr + (o.gated ? kn / 2 : kn), o.dtype);
+                float y[8], v[8];
+                if (o.gated) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) { y[i] = at(h + 2 * i); v[i] = at(h + 2 * i + 1); }
+                    if (o.bias) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) { y[i] += __ldg(o.bias + j + i); v[i] += __ldg(o.bias + o.K + j + i); }
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) { y[i] = at((h + 8 * s + i) % CW); v[i] = 1.f; }
+                    if (o.bias) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) y[i] += __ldg(o.bias + j + i);
+                    }
+                }
+                finish8(o, r, j, y, v, res);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; i += 2)
+                if (h + i < CW) finish_pair(o, r, k0 + i, at((h + i) % CW), at((h + i + 1) % CW));
+        }
+    }
+}
+
+// With SWAP a lane has one column k of z for CW rows from r on; neighbouring lanes neighbouring columns.
+template <int CW>
+__device__ __forceinline__ void finish_column(const OutArgs &o, int r, int k, const float2 (&acc)[CW / 2])
+{
+    const int K = o.K, half = k & 1, j = o.gated ? k >> 1 : k;
+    const bool live = k < o.Kz;
+    const float bias = o.bias && live ? __ldg(o.bias + (o.gated && half ? K + j : j)) : 0.f;
+    const bool mine = live && !(o.gated && half);
+#pragma unroll
+    for (int i = 0; i < CW; i += 8) {
+        float y[8], res[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            res[e] = o.residual && mine && r + i + e < o.R ? out_load(o.residual, (r + i + e) * o.ldr + j, o.dtype) : 0.f;
+            y[e] = (e & 1 ? acc[(i + e) / 2].y : acc[(i + e) / 2].x) + bias;
+        }
+        if (o.gated) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = __shfl_down_sync(0xffffffffu, y[e], 1);
+            activate_all(y, o.act);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] *= v[e];
+        } else {
+            activate_all(y, o.act);
+        }
+        if (o.residual) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] += res[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (mine && r + i + e < o.R) out_store(o.y, (r + i + e) * o.ldy + j, y[e], o.dtype);
     }
 }
 
 template <int BN, bool SWAP>
 __device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, const WaitCtx &ctx, uint32_t tmem,
-                                              const float *scales, float *patch, float *partial, int half, int quarter,
+                                              const float *scales, float *partial, int half, int quarter,
                                               int lane, int row0, int col0, const Range &rg, int &slot, uint32_t &sphase)
 {
     using C = Cfg<BN>;
@@ -236,16 +375,8 @@ __device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, cons
         return true;
     }
     if (active) {
-#pragma unroll
-        for (int h = 0; h < CW; h += LD) {
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < LD; ++i)
-                patch[lane * PATCH_PITCH + i] = (h + i) & 1 ? acc[(h + i) / 2].y : acc[(h + i) / 2].x;
-            __syncwarp();
-            finish_patch<SWAP>(a.out, patch, row0 + quarter * 32, col0 + c0 + h, LD);
-        }
-        __syncwarp();
+        if constexpr (SWAP) finish_column<CW>(a.out, col0 + c0, row0 + quarter * 32 + lane, acc);
+        else finish_row<CW>(a.out, row0 + quarter * 32 + lane, col0 + c0, acc);
     }
     return true;
 }
@@ -257,8 +388,7 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     using C = Cfg<BN>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *tiles = ptx::align_smem<1024>(smem_raw);
-    float *patches = reinterpret_cast<float *>(tiles + (size_t)C::STAGES * C::STAGE_BYTES);
-    float *scales = patches + EPI_WARPS * PATCH_FLOATS;
+    float *scales = reinterpret_cast<float *>(tiles + (size_t)C::STAGES * C::STAGE_BYTES);
     Shared *sh = reinterpret_cast<Shared *>(scales + (size_t)NSLOT * C::SLOT_SCALE_FLOATS);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)blockIdx.x % a.split, first = (int)blockIdx.x / a.split, stride = (int)gridDim.x / a.split;
@@ -422,8 +552,7 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         const uint32_t tmem = tmem_base + ((uint32_t)(quarter * 32) << 16);
         for (int t = first; t < a.tiles; t += stride) {
             const int mt = t % a.MT, nt = t / a.MT;
-            if (!epilogue_tile<BN, SWAP>(sh, a, ctx, tmem, scales, patches + e * PATCH_FLOATS,
-                                         reinterpret_cast<float *>(tiles), e >> 2, quarter, lane, mt * BM, nt * BN, rg,
+            if (!epilogue_tile<BN, SWAP>(sh, a, ctx, tmem, scales, reinterpret_cast<float *>(tiles), e >> 2, quarter, lane, mt * BM, nt * BN, rg,
                                          slot, sphase))
                 break;
         }
@@ -441,12 +570,17 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                 int r0, c0, r1, c1;                 // the pair's places in the tile
                 if constexpr (SWAP) { r0 = 2 * (i % (BM / 2)); r1 = r0 + 1; c0 = c1 = col0 + i / (BM / 2); }
                 else { r0 = r1 = i / (share / 2); c0 = col0 + 2 * (i % (share / 2)); c1 = c0 + 1; }
-                float v0 = 0.f, v1 = 0.f;
-                for (int p = 0; p < a.split; ++p) {
-                    const uint32_t base = ptx::map_rank(mine, (uint32_t)p);
-                    v0 += ptx::ld_cluster(base + (uint32_t)((c0 * (BM + 1) + r0) * 4));
-                    v1 += ptx::ld_cluster(base + (uint32_t)((c1 * (BM + 1) + r1) * 4));
-                }
+                float w0[8], w1[8], v0 = 0.f, v1 = 0.f;
+#pragma unroll
+                for (int p = 0; p < 8; ++p)         // all loads on their way before the first addition
+                    if (p < a.split) {
+                        const uint32_t base = ptx::map_rank(mine, (uint32_t)p);
+                        w0[p] = ptx::ld_cluster(base + (uint32_t)((c0 * (BM + 1) + r0) * 4));
+                        w1[p] = ptx::ld_cluster(base + (uint32_t)((c1 * (BM + 1) + r1) * 4));
+                    }
+#pragma unroll
+                for (int p = 0; p < 8; ++p)
+                    if (p < a.split) { v0 += w0[p]; v1 += w1[p]; }
                 if constexpr (SWAP) finish_pair(a.out, nt * BN + c0, mt * BM + r0, v0, v1);
                 else finish_pair(a.out, mt * BM + r0, nt * BN + c0, v0, v1);
             }
@@ -633,6 +767,8 @@ wfq_status_t product(wfq_linear *l, const int8_t *xq, const float *sx, int rows,
     o.ldr = ldr; o.ldy = ldy;
     o.K = l->K; o.Kz = l->Kz; o.R = rows;
     o.act = l->act; o.gated = l->gated; o.dtype = (int)l->out_dtype;
+    const size_t e = elem_bytes(l->out_dtype);
+    o.vec = !misaligned(y, 16) && ldy * e % 16 == 0 && (!residual || (!misaligned(residual, 16) && ldr * e % 16 == 0));
     return to_status(launch_product(*l, xq, sx, rows, o, st, pdl));
 }
 
