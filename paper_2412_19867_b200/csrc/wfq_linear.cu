@@ -65,15 +65,17 @@ struct Shared {
     volatile int abort;
 };
 
-template <int BN>
+template <int BN, bool SWAP>
 struct Cfg {
-    static constexpr int STAGES = BN == 256 ? 4 : BN == 128 ? 6 : BN == 64 ? 8 : 10;
+    static constexpr int STAGES = BN == 256 ? 4 : BN == 128 ? 5 : BN == 64 ? (SWAP ? 8 : 7) : 10;
+    static constexpr int PATCH_COLS = BN == 256 ? 16 : 32;        // columns of z on their way out at a time
+    static constexpr int PATCH_BYTES = SWAP ? 0 : 32 * (PATCH_COLS + 4) * 4;      // of one epilogue warp
     static constexpr int B_BYTES = BN * BK;
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
     static constexpr int CG_MAX = SLOT_COLS / BN < 4 ? SLOT_COLS / BN : 4;      // pieces per chunk at most
     static constexpr int GROUP_SCALE_FLOATS = BM + BN;
     static constexpr int SLOT_SCALE_FLOATS = CG_MAX * GROUP_SCALE_FLOATS;
-    static constexpr size_t SMEM_BYTES = 1024 + (size_t)STAGES * STAGE_BYTES +
+    static constexpr size_t SMEM_BYTES = 1024 + (size_t)STAGES * STAGE_BYTES + EPI_WARPS * PATCH_BYTES +
                                          (size_t)NSLOT * SLOT_SCALE_FLOATS * 4 + sizeof(Shared);
     static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
     static_assert((size_t)BN * (BM + 1) * 4 <= (size_t)STAGES * STAGE_BYTES, "partial sums fit the stages");
@@ -96,7 +98,7 @@ struct MmaArgs {
     int rows, cols;            // (R, Kz), with SWAP (Kz, R)
     int tiles, MT;             // tiles, blocks of 128 rows
     int split;                 // CTAs per tile (cluster size)
-    int steps, gsteps, cg;     // MMA steps of 32 channels in all, per group; pieces per chunk
+    int steps, gsteps, cg;     // MMA steps of 32 channels in all, per group; pieces per chunk (as in issue())
     int *status;
     long long wait_cycles;
     int debug_skip_stage;
@@ -166,50 +168,67 @@ __device__ __forceinline__ void finish_pair(const OutArgs &o, int r, int k, floa
     }
 }
 
-// Eight values of y or the residual at once (`vec`: 16-byte aligned rows).
-struct Pack8 { uint32_t w[8]; };             // 16-bit types: the first four words
-__device__ __forceinline__ Pack8 load_pack(const void *p, long long i, int dtype)
+// N (4 or 8) consecutive values of y or the residual at once, aligned to their size up to 16 bytes.
+template <int N> struct Packed { uint32_t w[N]; };      // 16-bit types: the first half of it
+template <int N>
+__device__ __forceinline__ Packed<N> load_packed(const void *p, long long i, int dtype)
 {
-    Pack8 r;
-    const uint4 *q = reinterpret_cast<const uint4 *>(static_cast<const char *>(p) + i * (dtype == WFQ_F32 ? 4 : 2));
-    const uint4 u = q[0];
-    r.w[0] = u.x; r.w[1] = u.y; r.w[2] = u.z; r.w[3] = u.w;
+    Packed<N> r;
     if (dtype == WFQ_F32) {
-        const uint4 v = q[1];
-        r.w[4] = v.x; r.w[5] = v.y; r.w[6] = v.z; r.w[7] = v.w;
+        const uint4 *q = reinterpret_cast<const uint4 *>(static_cast<const float *>(p) + i);
+#pragma unroll
+        for (int e = 0; e < N / 4; ++e) {
+            const uint4 u = q[e];
+            r.w[4 * e] = u.x; r.w[4 * e + 1] = u.y; r.w[4 * e + 2] = u.z; r.w[4 * e + 3] = u.w;
+        }
+    } else {
+        const uint2 *q = reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p) + i);
+        if constexpr (N == 8) {
+            const uint4 u = *reinterpret_cast<const uint4 *>(q);
+            r.w[0] = u.x; r.w[1] = u.y; r.w[2] = u.z; r.w[3] = u.w;
+        } else {
+            const uint2 u = *q;
+            r.w[0] = u.x; r.w[1] = u.y;
+        }
     }
     return r;
 }
-__device__ __forceinline__ void add_pack(float (&y)[8], const Pack8 &r, int dtype)
+template <int N>
+__device__ __forceinline__ void add_packed(float (&y)[N], const Packed<N> &r, int dtype)
 {
     if (dtype == WFQ_F32) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] += __uint_as_float(r.w[i]);
+        for (int i = 0; i < N; ++i) y[i] += __uint_as_float(r.w[i]);
     } else if (dtype == WFQ_F16) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < N / 2; ++i) {
             const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&r.w[i]));
             y[2 * i] += f.x; y[2 * i + 1] += f.y;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < N / 2; ++i) {
             y[2 * i] += __uint_as_float(r.w[i] << 16);
             y[2 * i + 1] += __uint_as_float(r.w[i] & 0xffff0000u);
         }
     }
 }
-__device__ __forceinline__ void store_pack(void *p, long long i, const float (&y)[8], int dtype)
+template <int N>
+__device__ __forceinline__ void store_packed(void *p, long long i, const float (&y)[N], int dtype)
 {
-    uint4 *q = reinterpret_cast<uint4 *>(static_cast<char *>(p) + i * (dtype == WFQ_F32 ? 4 : 2));
     if (dtype == WFQ_F32) {
-        q[0] = make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
-        q[1] = make_uint4(__float_as_uint(y[4]), __float_as_uint(y[5]), __float_as_uint(y[6]), __float_as_uint(y[7]));
-    } else {
-        const int kind = dtype == WFQ_F16 ? 1 : 2;
-        q[0] = make_uint4(to_bits16x2(y[0], y[1], kind), to_bits16x2(y[2], y[3], kind), to_bits16x2(y[4], y[5], kind),
-                          to_bits16x2(y[6], y[7], kind));
+        float4 *q = reinterpret_cast<float4 *>(static_cast<float *>(p) + i);
+#pragma unroll
+        for (int e = 0; e < N / 4; ++e) q[e] = make_float4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
+        return;
     }
+    const int kind = dtype == WFQ_F16 ? 1 : 2;
+    uint32_t w[N / 2];
+#pragma unroll
+    for (int e = 0; e < N / 2; ++e) w[e] = to_bits16x2(y[2 * e], y[2 * e + 1], kind);
+    uint16_t *q = static_cast<uint16_t *>(p) + i;
+    if constexpr (N == 8) *reinterpret_cast<uint4 *>(q) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<uint2 *>(q) = make_uint2(w[0], w[1]);
 }
 
 template <int N>
@@ -227,83 +246,92 @@ __device__ __forceinline__ void activate_all(float (&z)[N], int act)
     }
 }
 
-// Eight outputs of one row from eight (gated: sixteen) columns of z: column j of y on, all of them inside K.
-__device__ __forceinline__ void finish8(const OutArgs &o, long long r, int j, float (&y)[8], const float (&v)[8], const Pack8 &res)
+// The code of an epilogue runs once per tile and streams through the instruction cache: what is unrolled over the columns
+// of a thread is kept to moving registers (a first version, unrolled as a whole, took 15 us for 128 columns).
+//
+// CW columns of z that a thread holds for row `row0 + lane`, from column k0 on: PATCH_COLS at a time through the warp's
+// patch of shared memory, so that lanes write neighbouring pieces of a row.  The pitch of 36 (20) floats keeps 16-byte
+// accesses of eight lanes on different banks.
+template <int CW, int COLS>
+__device__ __forceinline__ void finish_rows(const OutArgs &o, float *patch, int lane, int row0, int k0,
+                                            const float2 (&acc)[CW / 2])
 {
-    activate_all(y, o.act);
-    if (o.gated) {
+    constexpr int PITCH = COLS + 4, PIECES = COLS / 8;            // pieces of eight columns
+    constexpr int ROWS = 32 / PIECES;                             // rows per step
+    const int piece = lane % PIECES, r_in = lane / PIECES;
+#pragma unroll 1
+    for (int h = 0; h < CW; h += COLS) {
+        __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] *= v[i];
-    }
-    if (o.residual) add_pack(y, res, o.dtype);
-    store_pack(o.y, r * o.ldy + j, y, o.dtype);
-}
-
-// CW columns of z that a thread holds for row r, from column k on.
-template <int CW>
-__device__ __forceinline__ void finish_row(const OutArgs &o, int r, int k, const float2 (&acc)[CW / 2])
-{
-    if (r >= o.R) return;
-    auto at = [&](int i) { return i & 1 ? acc[i / 2].y : acc[i / 2].x; };
-    const int step = o.gated ? 16 : 8;
-    const Pack8 none = {};
-    Pack8 next = o.vec && o.residual && k + step <= o.Kz ? load_pack(o.residual, r * o.ldr + (o.gated ? k / 2 : k), o.dtype)
-                                                         : none;
+        for (int c = 0; c < CW; c += COLS)
+            if (h == c) {
 #pragma unroll
-    for (int h = 0; h < CW; h += 16) {
-        const int k0 = k + h;
-        if (o.vec && k0 + 16 <= o.Kz) {
+                for (int i = 0; i < COLS; i += 4)
+                    *reinterpret_cast<float4 *>(patch + lane * PITCH + i) =
+                        make_float4(acc[(c + i) / 2].x, acc[(c + i) / 2].y, acc[(c + i) / 2 + 1].x, acc[(c + i) / 2 + 1].y);
+            }
+        __syncwarp();
+        const int k = k0 + h + 8 * piece;                         // first column of this lane's piece
+        if (o.vec && k + 8 <= o.Kz) {
+            const int j = o.gated ? k / 2 : k;
+            float b[8];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                if (s == 1 && o.gated) break;
-                const int j = o.gated ? k0 / 2 : k0 + 8 * s;
-                const Pack8 res = next;
-                // the next eight, ahead of this store (y may be the residual, element by element)
-                const int kn = o.gated ? k0 + 16 : k0 + 8 * (s + 1);
-                if (o.residual && kn < k + CW && kn + step <= o.Kz)
-                    next = load_pack(o.residual, r * o.ldr + (o.gated ? kn / 2 : kn), o.dtype);
-                float y[8], v[8];
+            for (int i = 0; i < 8; ++i)
+                b[i] = !o.bias ? 0.f : o.gated ? __ldg(o.bias + (i & 1 ? o.K : 0) + j + i / 2) : __ldg(o.bias + j + i);
+#pragma unroll 1
+            for (int q = 0; q < 32; q += ROWS) {
+                const long long r = row0 + q + r_in;
+                if (r >= o.R) continue;
+                float z[8];
+                const float4 *src = reinterpret_cast<const float4 *>(patch + (q + r_in) * PITCH + 8 * piece);
+                const float4 lo = src[0], hi = src[1];
+                z[0] = lo.x + b[0]; z[1] = lo.y + b[1]; z[2] = lo.z + b[2]; z[3] = lo.w + b[3];
+                z[4] = hi.x + b[4]; z[5] = hi.y + b[5]; z[6] = hi.z + b[6]; z[7] = hi.w + b[7];
                 if (o.gated) {
+                    float y[4] = {z[0], z[2], z[4], z[6]};
+                    activate_all(y, o.act);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) { y[i] = at(h + 2 * i); v[i] = at(h + 2 * i + 1); }
-                    if (o.bias) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) { y[i] += __ldg(o.bias + j + i); v[i] += __ldg(o.bias + o.K + j + i); }
-                    }
+                    for (int i = 0; i < 4; ++i) y[i] *= z[2 * i + 1];
+                    if (o.residual) add_packed(y, load_packed<4>(o.residual, r * o.ldr + j, o.dtype), o.dtype);
+                    store_packed(o.y, r * o.ldy + j, y, o.dtype);
                 } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) { y[i] = at((h + 8 * s + i) % CW); v[i] = 1.f; }
-                    if (o.bias) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) y[i] += __ldg(o.bias + j + i);
-                    }
+                    activate_all(z, o.act);
+                    if (o.residual) add_packed(z, load_packed<8>(o.residual, r * o.ldr + j, o.dtype), o.dtype);
+                    store_packed(o.y, r * o.ldy + j, z, o.dtype);
                 }
-                finish8(o, r, j, y, v, res);
             }
         } else {
-#pragma unroll
-            for (int i = 0; i < 16; i += 2)
-                if (h + i < CW) finish_pair(o, r, k0 + i, at((h + i) % CW), at((h + i + 1) % CW));
+#pragma unroll 1
+            for (int q = 0; q < 32; q += ROWS)
+#pragma unroll 1
+                for (int i = 0; i < 8; i += 2) {
+                    const float *src = patch + (q + r_in) * PITCH + 8 * piece + i;
+                    finish_pair(o, row0 + q + r_in, k + i, src[0], src[1]);
+                }
         }
     }
 }
 
-// With SWAP a lane has one column k of z for CW rows from r on; neighbouring lanes neighbouring columns.
+// With SWAP a lane has one column k of z for CW rows from r0 on; neighbouring lanes neighbouring columns.
 template <int CW>
-__device__ __forceinline__ void finish_column(const OutArgs &o, int r, int k, const float2 (&acc)[CW / 2])
+__device__ __forceinline__ void finish_columns(const OutArgs &o, int r0, int k, const float2 (&acc)[CW / 2])
 {
-    const int K = o.K, half = k & 1, j = o.gated ? k >> 1 : k;
-    const bool live = k < o.Kz;
-    const float bias = o.bias && live ? __ldg(o.bias + (o.gated && half ? K + j : j)) : 0.f;
-    const bool mine = live && !(o.gated && half);
-#pragma unroll
-    for (int i = 0; i < CW; i += 8) {
+    const int half = k & 1, j = o.gated ? k >> 1 : k;
+    const bool live = k < o.Kz, mine = live && !(o.gated && half);
+    const float bias = o.bias && live ? __ldg(o.bias + (o.gated && half ? o.K + j : j)) : 0.f;
+#pragma unroll 1
+    for (int h = 0; h < CW; h += 8) {
         float y[8], res[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            res[e] = o.residual && mine && r + i + e < o.R ? out_load(o.residual, (r + i + e) * o.ldr + j, o.dtype) : 0.f;
-            y[e] = (e & 1 ? acc[(i + e) / 2].y : acc[(i + e) / 2].x) + bias;
-        }
+        for (int c = 0; c < CW; c += 8)
+            if (h == c) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = (e & 1 ? acc[(c + e) / 2].y : acc[(c + e) / 2].x) + bias;
+            }
+        const int r = r0 + h;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            res[e] = o.residual && mine && r + e < o.R ? out_load(o.residual, (r + e) * o.ldr + j, o.dtype) : 0.f;
         if (o.gated) {
             float v[8];
 #pragma unroll
@@ -320,16 +348,16 @@ __device__ __forceinline__ void finish_column(const OutArgs &o, int r, int k, co
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (mine && r + i + e < o.R) out_store(o.y, (r + i + e) * o.ldy + j, y[e], o.dtype);
+            if (mine && r + e < o.R) out_store(o.y, (r + e) * o.ldy + j, y[e], o.dtype);
     }
 }
 
 template <int BN, bool SWAP>
 __device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, const WaitCtx &ctx, uint32_t tmem,
-                                              const float *scales, float *partial, int half, int quarter,
+                                              const float *scales, float *patch, float *partial, int half, int quarter,
                                               int lane, int row0, int col0, const Range &rg, int &slot, uint32_t &sphase)
 {
-    using C = Cfg<BN>;
+    using C = Cfg<BN, SWAP>;
     constexpr int CW = BN / 2;                    // columns of a warp
     constexpr int LD = CW < 16 ? CW : 16;         // columns of one tensor-memory load
     const int c0 = half * CW;
@@ -348,17 +376,25 @@ __device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, cons
                 const float rs = sc[j * C::GROUP_SCALE_FLOATS + quarter * 32 + lane];
                 const float2 rs2 = make_float2(rs, rs);
                 const float *cs = sc + j * C::GROUP_SCALE_FLOATS + BM + c0;
+uint32_t rr[2][LD];
+                auto fetch = [&](int h) {
+                    if constexpr (LD == 16) ptx::tmem_ld_x16(taddr + (uint32_t)(LD * h), rr[h & 1]);
+                    else ptx::tmem_ld_x8(taddr + (uint32_t)(LD * h), rr[h & 1]);
+                };
+                fetch(0);
 #pragma unroll
-                for (int h = 0; h < CW / LD; ++h) {
-                    uint32_t r[LD];
-                    if constexpr (LD == 16) ptx::tmem_ld_x16(taddr + (uint32_t)(LD * h), r);
-                    else ptx::tmem_ld_x8(taddr + (uint32_t)(LD * h), r);
+                for (int h = 0; h < CW / LD; ++h) {              // the next columns on their way
+                    uint32_t (&r)[LD] = rr[h & 1];
                     ptx::tmem_ld_wait(r);
+                    if (h + 1 < CW / LD) fetch(h + 1);
 #pragma unroll
-                    for (int i = 0; i < LD; i += 2) {
-                        const float2 c2 = *reinterpret_cast<const float2 *>(cs + LD * h + i);
-                        const float2 f = make_float2(__int2float_rn((int)r[i]), __int2float_rn((int)r[i + 1]));
-                        acc[(LD * h + i) / 2] = __ffma2_rn(__fmul2_rn(f, rs2), c2, acc[(LD * h + i) / 2]);
+                    for (int i = 0; i < LD; i += 4) {
+                        const float4 c4 = *reinterpret_cast<const float4 *>(cs + LD * h + i);
+                        const int k = (LD * h + i) / 2;
+                        const float2 f0 = make_float2(__int2float_rn((int)r[i]), __int2float_rn((int)r[i + 1]));
+                        const float2 f1 = make_float2(__int2float_rn((int)r[i + 2]), __int2float_rn((int)r[i + 3]));
+                        acc[k] = __ffma2_rn(__fmul2_rn(f0, rs2), make_float2(c4.x, c4.y), acc[k]);
+                        acc[k + 1] = __ffma2_rn(__fmul2_rn(f1, rs2), make_float2(c4.z, c4.w), acc[k + 1]);
                     }
                 }
             }
@@ -375,20 +411,116 @@ __device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, cons
         return true;
     }
     if (active) {
-        if constexpr (SWAP) finish_column<CW>(a.out, col0 + c0, row0 + quarter * 32 + lane, acc);
-        else finish_row<CW>(a.out, row0 + quarter * 32 + lane, col0 + c0, acc);
+        if constexpr (SWAP) finish_columns<CW>(a.out, col0 + c0, row0 + quarter * 32 + lane, acc);
+        else finish_rows<CW, C::PATCH_COLS>(a.out, patch, lane, row0 + quarter * 32, col0 + c0, acc);
     }
     return true;
+}
+
+// The MMA issuer's loop.  GST: steps of 32 channels per group, 4 standing for any multiple of four (groups begin and end
+// with a stage), 0 for every other number.  Its instructions form one dependent chain: with the place of a step in its
+// group decided at run time a stage of four MMAs took 1270 cycles.
+template <int BN, bool SWAP, int GST>
+__device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tmem_base, const MmaArgs &a, const Range &rg,
+                                      const WaitCtx &ctx, int first, int stride)
+{
+    using C = Cfg<BN, SWAP>;
+    constexpr uint32_t dhi = ptx::smem_desc_sw128_hi();
+    constexpr uint32_t idesc = ptx::idesc_i8(BM, BN);
+    constexpr int PER = GST == 1 || GST == 2 ? 4 / GST : 1;              // groups per stage
+    constexpr int CG = PER < C::CG_MAX ? PER : C::CG_MAX;                // pieces per chunk
+    const uint32_t full0 = ptx::smem_u32(&sh->full[0]), empty0 = ptx::smem_u32(&sh->empty[0]);
+    const uint32_t acc0 = ptx::smem_u32(&sh->acc_full[0]), free0 = ptx::smem_u32(&sh->slot_free[0]);
+    int stage = 0, slot = 0;
+    uint32_t phase = 0, sphase = 0;
+    for (int t = first; t < a.tiles; t += stride) {
+        int in_group = rg.s0 % a.gsteps;                                 // GST 4 and 0: steps into the current group
+        bool begins = true;                                              // the next step is the first of its piece
+        for (int kb = rg.kb0; kb < rg.kb1; ++kb) {
+            const int n = min(4, rg.s1 - 4 * kb);
+            if (!wait_warp(full0 + 8u * stage, phase, ctx, kWaitSmemFull)) return;
+            const uint32_t a_lo = tiles_lo + (uint32_t)(stage * (C::STAGE_BYTES >> 4));
+            const uint32_t b_lo = a_lo + (uint32_t)(A_BYTES >> 4);
+            if constexpr (GST == 4) {
+                if (begins && !wait_warp(free0 + 8u * slot, sphase ^ 1u, ctx, kWaitTmemEmpty)) return;
+                in_group += n;
+                const bool ends = in_group == a.gsteps || 4 * kb + n == rg.s1;
+                ptx::tc_fence_after();
+                if (ptx::elect_one()) {
+                    const uint32_t d = tmem_base + (uint32_t)(slot * SLOT_COLS);
+                    ptx::umma_i8_lo(d, a_lo, b_lo, dhi, idesc, !begins);
+                    if (n > 1) ptx::umma_i8_lo<true>(d, a_lo + 2, b_lo + 2, dhi, idesc);
+                    if (n > 2) ptx::umma_i8_lo<true>(d, a_lo + 4, b_lo + 4, dhi, idesc);
+                    if (n > 3) ptx::umma_i8_lo<true>(d, a_lo + 6, b_lo + 6, dhi, idesc);
+                    ptx::umma_commit(empty0 + 8u * stage);
+                    if (ends) ptx::umma_commit(acc0 + 8u * slot);
+                }
+                __syncwarp();
+                begins = ends;
+                if (ends) {
+                    in_group = 0;
+                    if (++slot == NSLOT) { slot = 0; sphase ^= 1u; }
+                }
+            } else if constexpr (GST > 0) {
+#pragma unroll
+                for (int c = 0; c < 4; c += CG * GST) {                  // chunks of the stage
+                    if (c < n) {
+                        if (!wait_warp(free0 + 8u * slot, sphase ^ 1u, ctx, kWaitTmemEmpty)) return;
+                        ptx::tc_fence_after();
+                        if (ptx::elect_one()) {
+                            const uint32_t d = tmem_base + (uint32_t)(slot * SLOT_COLS);
+#pragma unroll
+                            for (int s = c; s < c + CG * GST; ++s)
+                                if (s < n) {
+                                    const uint32_t dj = d + (uint32_t)((s - c) / GST * BN), off = 2u * s;
+                                    if (s % GST) ptx::umma_i8_lo<true>(dj, a_lo + off, b_lo + off, dhi, idesc);
+                                    else ptx::umma_i8_lo<false>(dj, a_lo + off, b_lo + off, dhi, idesc);
+                                }
+                            ptx::umma_commit(acc0 + 8u * slot);
+                        }
+                        __syncwarp();
+                        if (++slot == NSLOT) { slot = 0; sphase ^= 1u; }
+                    }
+                }
+                if (ptx::elect_one()) ptx::umma_commit(empty0 + 8u * stage);
+                __syncwarp();
+            } else {
+                ptx::tc_fence_after();
+                for (int s = 0; s < n; ++s) {
+                    if (begins) {
+                        if (!wait_warp(free0 + 8u * slot, sphase ^ 1u, ctx, kWaitTmemEmpty)) return;
+                        ptx::tc_fence_after();
+                    }
+                    const bool ends = ++in_group == a.gsteps || 4 * kb + s + 1 == rg.s1;
+                    if (ptx::elect_one()) {
+                        const uint32_t d = tmem_base + (uint32_t)(slot * SLOT_COLS);
+                        ptx::umma_i8_lo(d, a_lo + 2 * s, b_lo + 2 * s, dhi, idesc, !begins);
+                        if (ends) ptx::umma_commit(acc0 + 8u * slot);
+                    }
+                    __syncwarp();
+                    begins = ends;
+                    if (ends) {
+                        in_group = 0;
+                        if (++slot == NSLOT) { slot = 0; sphase ^= 1u; }
+                    }
+                }
+                if (ptx::elect_one()) ptx::umma_commit(empty0 + 8u * stage);
+                __syncwarp();
+            }
+            if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+        }
+    }
 }
 
 template <int BN, bool SWAP>
 __global__ void __launch_bounds__(THREADS, 1)
 linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, MmaArgs a)
 {
-    using C = Cfg<BN>;
+    using C = Cfg<BN, SWAP>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *tiles = ptx::align_smem<1024>(smem_raw);
-    float *scales = reinterpret_cast<float *>(tiles + (size_t)C::STAGES * C::STAGE_BYTES);
+    float *patches = reinterpret_cast<float *>(tiles + (size_t)C::STAGES * C::STAGE_BYTES);
+    float *scales = patches + EPI_WARPS * (C::PATCH_BYTES / 4);
     Shared *sh = reinterpret_cast<Shared *>(scales + (size_t)NSLOT * C::SLOT_SCALE_FLOATS);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)blockIdx.x % a.split, first = (int)blockIdx.x / a.split, stride = (int)gridDim.x / a.split;
@@ -458,55 +590,11 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         }
     } else if (warp == 1) {
         // ---------------- MMA issuer ----------------
-        constexpr uint32_t dhi = ptx::smem_desc_sw128_hi();
-        constexpr uint32_t idesc = ptx::idesc_i8(BM, BN);
         const uint32_t tiles_lo = ptx::smem_desc_sw128_lo(ptx::smem_u32(tiles));
-        int stage = 0, slot = 0;
-        uint32_t phase = 0, sphase = 0;
-        bool ok = true;
-        for (int t = first; t < a.tiles && ok; t += stride) {
-            int in_chunk = 0;                       // pieces of the current chunk that are complete
-            int in_group = rg.s0 % a.gsteps;        // steps into the current group
-            bool fresh = true;                      // the next step is the first of its piece
-            uint32_t dcol = 0;
-            for (int kb = rg.kb0; kb < rg.kb1 && ok; ++kb) {
-                ok = wait_warp(ptx::smem_u32(&sh->full[stage]), phase, ctx, kWaitSmemFull);
-                if (!ok) break;
-                ptx::tc_fence_after();
-                const uint32_t a_lo = tiles_lo + (uint32_t)(stage * (C::STAGE_BYTES >> 4));
-                const uint32_t b_lo = a_lo + (uint32_t)(A_BYTES >> 4);
-                const int n = min(4, rg.s1 - 4 * kb);
-                for (int s = 0; s < n; ++s) {
-                    if (fresh && in_chunk == 0) {
-                        ok = wait_warp(ptx::smem_u32(&sh->slot_free[slot]), sphase ^ 1u, ctx, kWaitTmemEmpty);
-                        if (!ok) break;
-                        ptx::tc_fence_after();
-                        dcol = tmem_base + (uint32_t)(slot * SLOT_COLS);
-                    }
-                    if (ptx::elect_one()) {
-                        if (fresh) ptx::umma_i8_lo<false>(dcol, a_lo + 2 * s, b_lo + 2 * s, dhi, idesc);
-                        else ptx::umma_i8_lo<true>(dcol, a_lo + 2 * s, b_lo + 2 * s, dhi, idesc);
-                    }
-                    __syncwarp();
-                    fresh = false;
-                    if (++in_group == a.gsteps || 4 * kb + s + 1 == rg.s1) {
-                        in_group = 0;
-                        fresh = true;
-                        dcol += BN;
-                        if (++in_chunk == a.cg || 4 * kb + s + 1 == rg.s1) {
-                            if (ptx::elect_one()) ptx::umma_commit(ptx::smem_u32(&sh->acc_full[slot]));
-                            __syncwarp();
-                            in_chunk = 0;
-                            if (++slot == NSLOT) { slot = 0; sphase ^= 1u; }
-                        }
-                    }
-                }
-                if (!ok) break;
-                if (ptx::elect_one()) ptx::umma_commit(ptx::smem_u32(&sh->empty[stage]));
-                __syncwarp();
-                if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
-            }
-        }
+        if (a.gsteps % 4 == 0 || a.gsteps >= a.steps) issue<BN, SWAP, 4>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
+        else if (a.gsteps == 2) issue<BN, SWAP, 2>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
+        else if (a.gsteps == 1) issue<BN, SWAP, 1>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
+        else issue<BN, SWAP, 0>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
     } else if (warp == 2) {
         // ---------------- scale loader ----------------
         int slot = 0;
@@ -552,7 +640,8 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         const uint32_t tmem = tmem_base + ((uint32_t)(quarter * 32) << 16);
         for (int t = first; t < a.tiles; t += stride) {
             const int mt = t % a.MT, nt = t / a.MT;
-            if (!epilogue_tile<BN, SWAP>(sh, a, ctx, tmem, scales, reinterpret_cast<float *>(tiles), e >> 2, quarter, lane, mt * BM, nt * BN, rg,
+            if (!epilogue_tile<BN, SWAP>(sh, a, ctx, tmem, scales, patches + e * (C::PATCH_BYTES / 4),
+                                         reinterpret_cast<float *>(tiles), e >> 2, quarter, lane, mt * BM, nt * BN, rg,
                                          slot, sphase))
                 break;
         }
@@ -644,7 +733,7 @@ template <int BN, bool SWAP>
 cudaError_t setup_variant()
 {
     return cudaFuncSetAttribute(linear_mma_kernel<BN, SWAP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                (int)Cfg<BN>::SMEM_BYTES);
+                                (int)Cfg<BN, SWAP>::SMEM_BYTES);
 }
 
 template <int BN, bool SWAP>
@@ -652,14 +741,14 @@ cudaError_t launch_variant(const wfq_linear &l, MmaArgs &a, int grid, const int8
                            bool pdl)
 {
     a.cg = 1;
-    if (BK % l.gs == 0) a.cg = BK / l.gs < Cfg<BN>::CG_MAX ? BK / l.gs : Cfg<BN>::CG_MAX;
+    if (BK % l.gs == 0) a.cg = BK / l.gs < Cfg<BN, SWAP>::CG_MAX ? BK / l.gs : Cfg<BN, SWAP>::CG_MAX;
     CUtensorMap tx, tw;
     if (!encode_codes(&tx, xq, l.Cp, rows, SWAP ? BN : BM) || !encode_codes(&tw, l.Wq, l.Cp, l.Kz, SWAP ? BM : BN))
         return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = Cfg<BN>::SMEM_BYTES;
+    cfg.dynamicSmemBytes = Cfg<BN, SWAP>::SMEM_BYTES;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     int n = 0;

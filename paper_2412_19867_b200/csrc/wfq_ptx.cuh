@@ -261,6 +261,17 @@ __device__ __forceinline__ void umma_i8_lo(uint32_t d_tmem, uint32_t a_lo, uint3
             ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(desc_hi), "r"(idesc));
     }
 }
+// With the accumulate flag at run time.
+__device__ __forceinline__ void umma_i8_lo(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t desc_hi,
+                                           uint32_t idesc, bool accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .b64 da, db;\n\t.reg .pred p;\n\t"
+        "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::i8 [%0], da, db, %4, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(desc_hi), "r"(idesc), "r"((uint32_t)accumulate));
+}
 // D[tmem] (+)= A[smem] * B[smem], fp16 x fp16 -> fp32 (K = 16 per instruction), descriptors
 // given as for umma_i8_lo.
 template <bool ACCUMULATE>
