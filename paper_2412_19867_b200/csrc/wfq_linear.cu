@@ -4,10 +4,12 @@
 //
 // linear_mma_kernel: persistent, warp-specialised, one CTA per SM.  A tile is 128 rows x BN columns of z; "rows" are the
 // 128 TMEM lanes of the accumulator: rows of x, or with SWAP output channels (few rows of x, so that all lanes carry
-// work).  Gated weights are stored with gate and value channels alternating, so that a pair is two neighbours.
+// work).  With PAIR two CTAs share a tile of 256 rows (tcgen05.mma.cta_group::2): each loads its 128 rows and half of the
+// columns' operand.  Gated weights are stored with gate and value channels alternating, so that a pair is two neighbours.
 //   warp 0      TMA producer: 128 channels of both operands per stage (128-byte swizzle)
-//   warp 1      allocates TMEM, issues tcgen05.mma kind::i8 (K = 32): a piece is the part of a group that this CTA has;
-//               pieces of a chunk (up to 128 channels where the group divides 128) lie side by side in one TMEM slot
+//   warp 1      allocates TMEM, issues tcgen05.mma kind::i8 (K = 32): a piece is a group, or up to 256 channels of a longer
+//               one, as far as this CTA has them; pieces of a chunk (up to 128 channels where the group divides 128) lie
+//               side by side in one TMEM slot
 //   warp 2      scale loader: 128 row scales and BN column scales per piece
 //   warps 4-11  epilogue: int32 sums to fp32, times the scales, into registers; then bias, activation, gate, residual
 // With few tiles a cluster of up to eight CTAs shares one: each takes a range of the channels, the partial sums are
@@ -60,26 +62,38 @@ constexpr int THREADS = 32 * (FIRST_EPI_WARP + EPI_WARPS);
 struct Shared {
     uint64_t full[16], empty[16];
     uint64_t acc_full[NSLOT], slot_free[NSLOT];
+    uint64_t scale_free[NSLOT];      // PAIR: this CTA's epilogue is done with a slot (slot_free counts both CTAs')
     uint64_t mma_done;
     uint32_t tmem_base;
     volatile int abort;
 };
 
-template <int BN, bool SWAP>
+template <int BN, bool SWAP, bool PAIR>
 struct Cfg {
-    static constexpr int STAGES = BN == 256 ? 4 : BN == 128 ? 5 : BN == 64 ? (SWAP ? 8 : 7) : 10;
-    static constexpr int PATCH_COLS = BN == 256 ? 16 : 32;        // columns of z on their way out at a time
+    static_assert(!(SWAP && PAIR), "pairs: rows of x on the lanes");
+    static constexpr int B_ROWS = PAIR ? BN / 2 : BN;             // of the columns' operand in this CTA
+    static constexpr int STAGE_BYTES = A_BYTES + B_ROWS * BK;
+    static constexpr int STAGES = STAGE_BYTES > 24 * 1024 ? 5 : STAGE_BYTES > 20 * 1024 ? (SWAP ? 8 : 7) : 10;
+    static constexpr int PATCH_COLS = 32;                         // columns of z on their way out at a time
     static constexpr int PATCH_BYTES = SWAP ? 0 : 32 * (PATCH_COLS + 4) * 4;      // of one epilogue warp
-    static constexpr int B_BYTES = BN * BK;
-    static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
-    static constexpr int CG_MAX = SLOT_COLS / BN < 4 ? SLOT_COLS / BN : 4;      // pieces per chunk at most
+    static constexpr int CG_MAX = SLOT_COLS / BN < 4 ? SLOT_COLS / BN : 4;        // pieces per chunk at most
     static constexpr int GROUP_SCALE_FLOATS = BM + BN;
     static constexpr int SLOT_SCALE_FLOATS = CG_MAX * GROUP_SCALE_FLOATS;
     static constexpr size_t SMEM_BYTES = 1024 + (size_t)STAGES * STAGE_BYTES + EPI_WARPS * PATCH_BYTES +
                                          (size_t)NSLOT * SLOT_SCALE_FLOATS * 4 + sizeof(Shared);
     static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
-    static_assert((size_t)BN * (BM + 1) * 4 <= (size_t)STAGES * STAGE_BYTES, "partial sums fit the stages");
+    static_assert(PAIR || (size_t)BN * (BM + 1) * 4 <= (size_t)STAGES * STAGE_BYTES, "partial sums fit the stages");
+    // Registers behind setmaxnreg: the epilogue holds BN / 2 sums and two blocks of loads.
+    // 128 * 40 + 256 * 232 = 384 * 168, what the block is launched with.
+    static constexpr bool MOVE_REGS = PAIR && BN == 256;
 };
+
+template <typename C>
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, const WaitCtx &ctx, int where)
+{
+    if constexpr (C::MOVE_REGS) return wait_warp_inline(bar, parity, ctx, where);
+    else return wait_warp(bar, parity, ctx, where);
+}
 
 struct OutArgs {
     const float *bias;
@@ -96,9 +110,10 @@ struct MmaArgs {
     const float *row_scale, *col_scale;
     long long row_pitch, col_pitch;
     int rows, cols;            // (R, Kz), with SWAP (Kz, R)
-    int tiles, MT;             // tiles, blocks of 128 rows
-    int split;                 // CTAs per tile (cluster size)
+    int tiles, MT;             // tiles, blocks of 128 (PAIR: 256) rows
+    int split;                 // CTAs that share the channels of a tile (cluster size; 1 with PAIR)
     int steps, gsteps, cg;     // MMA steps of 32 channels in all, per group; pieces per chunk (as in issue())
+    int ppg;                   // pieces per group
     int *status;
     long long wait_cycles;
     int debug_skip_stage;
@@ -106,8 +121,14 @@ struct MmaArgs {
     OutArgs out;
 };
 
-// The channels of this CTA: stages, steps and the pieces (parts of groups) that they fall into.
-struct Range { int kb0, kb1, s0, s1, g0, np; };
+// The channels of this CTA: stages, steps and pieces.  A group's pieces are PIECE steps long but the last one, wherever
+// the CTAs' ranges begin.
+constexpr int PIECE = 8;
+struct Range { int kb0, kb1, s0, s1, p0, np; };
+__device__ __forceinline__ int piece_of(const MmaArgs &a, int step)
+{
+    return step / a.gsteps * a.ppg + step % a.gsteps / PIECE;
+}
 __device__ __forceinline__ Range range_of(const MmaArgs &a, int rank)
 {
     Range r;
@@ -116,8 +137,8 @@ __device__ __forceinline__ Range range_of(const MmaArgs &a, int rank)
     r.kb1 = (int)((long long)KB * (rank + 1) / a.split);
     r.s0 = 4 * r.kb0;
     r.s1 = min(a.steps, 4 * r.kb1);
-    r.g0 = r.s0 / a.gsteps;
-    r.np = (r.s1 - 1) / a.gsteps - r.g0 + 1;
+    r.p0 = piece_of(a, r.s0);
+    r.np = piece_of(a, r.s1 - 1) - r.p0 + 1;
     return r;
 }
 
@@ -352,67 +373,140 @@ __device__ __forceinline__ void finish_columns(const OutArgs &o, int r0, int k, 
     }
 }
 
-template <int BN, bool SWAP>
-__device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, const WaitCtx &ctx, uint32_t tmem,
-                                              const float *scales, float *patch, float *partial, int half, int quarter,
-                                              int lane, int row0, int col0, const Range &rg, int &slot, uint32_t &sphase)
+// Sums in tensor memory start from the bit pattern of 1.5 * 2^23 instead of zero (MAGIC): read as a float, pattern + sum is
+// 1.5 * 2^23 + sum exactly for |sum| < 2^22, and 127 * 127 * 256 is below that.  The conversion and the product with the row
+// scale are then one multiply-add, f * rs - 1.5 * 2^23 * rs, which is sum * rs rounded once where the second product is
+// exact: the row scale is rounded to 22 bits for that (2^-23 of it at most).  The epilogue writes the pattern back behind
+// its reads.  Against conversions (64 a clock and SM) and two products it halves the issue slots per sum.
+constexpr uint32_t kMagicBits = 0x4b400000u;
+constexpr float kMagic = 12582912.f;
+// With SWAP (few rows of x, bound by the weights' bytes) sums are converted.
+template <bool SWAP> constexpr bool kUseMagic = !SWAP;
+
+__device__ __forceinline__ float round22(float s)
 {
-    using C = Cfg<BN, SWAP>;
+    const uint32_t u = __float_as_uint(s);
+    return s < 3e38f ? __uint_as_float((u + 1 + ((u >> 2) & 1)) & ~3u) : s;      // to nearest even; scales are not negative
+}
+
+// One piece: CW columns of a lane's row, 16 at a time with the next 16 on their way.  BIG: row scales whose product with
+// 1.5 * 2^23 could overflow.
+template <int CW, bool MAGIC, bool BIG>
+__device__ __forceinline__ void promote(uint32_t taddr, float rs, const float *cs, float2 (&acc)[CW / 2])
+{
+    constexpr int LD = CW < 16 ? CW : 16;
+    const float2 rs2 = make_float2(rs, rs);
+    const float off = -kMagic * rs;
+    const float2 off2 = make_float2(off, off), magic2 = make_float2(-kMagic, -kMagic);
+    uint32_t rr[2][LD];
+    auto fetch = [&](int h) {
+        if constexpr (LD == 16) ptx::tmem_ld_x16(taddr + (uint32_t)(LD * h), rr[h & 1]);
+        else ptx::tmem_ld_x8(taddr + (uint32_t)(LD * h), rr[h & 1]);
+    };
+    uint32_t pattern[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) pattern[i] = kMagicBits;
+    fetch(0);
+#pragma unroll
+    for (int h = 0; h < CW / LD; ++h) {
+        uint32_t (&r)[LD] = rr[h & 1];
+        ptx::tmem_ld_wait(r);
+        if (h + 1 < CW / LD) fetch(h + 1);
+        if constexpr (MAGIC) {
+#pragma unroll
+            for (int i = 0; i < LD; i += 8) ptx::tmem_st_x8(taddr + (uint32_t)(LD * h + i), pattern);
+        }
+#pragma unroll
+        for (int i = 0; i < LD; i += 4) {
+            const float4 c4 = *reinterpret_cast<const float4 *>(cs + LD * h + i);
+            const int k = (LD * h + i) / 2;
+            float2 f0, f1;
+            if constexpr (MAGIC) {
+                f0 = make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
+                f1 = make_float2(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+                if constexpr (BIG) {
+                    f0 = __fmul2_rn(__fadd2_rn(f0, magic2), rs2);
+                    f1 = __fmul2_rn(__fadd2_rn(f1, magic2), rs2);
+                } else {
+                    f0 = __ffma2_rn(f0, rs2, off2);
+                    f1 = __ffma2_rn(f1, rs2, off2);
+                }
+            } else {
+                f0 = __fmul2_rn(make_float2(__int2float_rn((int)r[i]), __int2float_rn((int)r[i + 1])), rs2);
+                f1 = __fmul2_rn(make_float2(__int2float_rn((int)r[i + 2]), __int2float_rn((int)r[i + 3])), rs2);
+            }
+            acc[k] = __ffma2_rn(f0, make_float2(c4.x, c4.y), acc[k]);
+            acc[k + 1] = __ffma2_rn(f1, make_float2(c4.z, c4.w), acc[k + 1]);
+        }
+    }
+}
+
+// What an epilogue warp keeps through the kernel.
+struct EpiCtx {
+    uint32_t tmem;               // its lanes and first column in tensor memory
+    const float *scales;
+    float *patch, *partial;
+    uint32_t free_bar;           // slot_free[0]: this CTA's, or with PAIR the leader's
+    int c0, quarter, lane;       // first column of the tile that is this warp's
+};
+
+template <int BN, bool SWAP, bool PAIR>
+__device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, const WaitCtx &ctx, const EpiCtx &ec, int row0,
+                                              int col0, const Range &rg, int &slot, uint32_t &sphase)
+{
+    using C = Cfg<BN, SWAP, PAIR>;
+    constexpr bool MAGIC = kUseMagic<SWAP>;
     constexpr int CW = BN / 2;                    // columns of a warp
-    constexpr int LD = CW < 16 ? CW : 16;         // columns of one tensor-memory load
-    const int c0 = half * CW;
-    const bool active = row0 + quarter * 32 < a.rows && col0 + c0 < a.cols;
+    const int quarter = ec.quarter, lane = ec.lane;
+    // A warp without rows or columns of z still writes the pattern back
+    const bool active = row0 + quarter * 32 < a.rows && col0 + ec.c0 < a.cols;
     float2 acc[CW / 2];
 #pragma unroll
     for (int j = 0; j < CW / 2; ++j) acc[j] = make_float2(0.f, 0.f);
     for (int q0 = 0; q0 < rg.np; q0 += a.cg) {
         const int n = min(a.cg, rg.np - q0);
-        if (!wait_warp(ptx::smem_u32(&sh->acc_full[slot]), sphase, ctx, kWaitTmemFull)) return false;
-        if (active) {
-            ptx::tc_fence_after();
-            const float *sc = scales + (size_t)slot * C::SLOT_SCALE_FLOATS;
+        if (!wait<C>(ptx::smem_u32(&sh->acc_full[slot]), sphase, ctx, kWaitTmemFull)) return false;
+        ptx::tc_fence_after();
+        if (active || MAGIC) {
+            const float *sc = ec.scales + (size_t)slot * C::SLOT_SCALE_FLOATS;
             for (int j = 0; j < n; ++j) {
-                const uint32_t taddr = tmem + (uint32_t)(slot * SLOT_COLS + j * BN + c0);
-                const float rs = sc[j * C::GROUP_SCALE_FLOATS + quarter * 32 + lane];
-                const float2 rs2 = make_float2(rs, rs);
-                const float *cs = sc + j * C::GROUP_SCALE_FLOATS + BM + c0;
-uint32_t rr[2][LD];
-                auto fetch = [&](int h) {
-                    if constexpr (LD == 16) ptx::tmem_ld_x16(taddr + (uint32_t)(LD * h), rr[h & 1]);
-                    else ptx::tmem_ld_x8(taddr + (uint32_t)(LD * h), rr[h & 1]);
-                };
-                fetch(0);
-#pragma unroll
-                for (int h = 0; h < CW / LD; ++h) {              // the next columns on their way
-                    uint32_t (&r)[LD] = rr[h & 1];
-                    ptx::tmem_ld_wait(r);
-                    if (h + 1 < CW / LD) fetch(h + 1);
-#pragma unroll
-                    for (int i = 0; i < LD; i += 4) {
-                        const float4 c4 = *reinterpret_cast<const float4 *>(cs + LD * h + i);
-                        const int k = (LD * h + i) / 2;
-                        const float2 f0 = make_float2(__int2float_rn((int)r[i]), __int2float_rn((int)r[i + 1]));
-                        const float2 f1 = make_float2(__int2float_rn((int)r[i + 2]), __int2float_rn((int)r[i + 3]));
-                        acc[k] = __ffma2_rn(__fmul2_rn(f0, rs2), make_float2(c4.x, c4.y), acc[k]);
-                        acc[k + 1] = __ffma2_rn(__fmul2_rn(f1, rs2), make_float2(c4.z, c4.w), acc[k + 1]);
-                    }
+                const uint32_t taddr = ec.tmem + (uint32_t)(slot * SLOT_COLS + j * BN);
+                const float *cs = sc + j * C::GROUP_SCALE_FLOATS + BM + ec.c0;
+                float rs = sc[j * C::GROUP_SCALE_FLOATS + quarter * 32 + lane];
+                if constexpr (MAGIC) {
+                    rs = round22(rs);
+                    if (__any_sync(0xffffffffu, !(rs < 1e30f))) promote<CW, true, true>(taddr, rs, cs, acc);
+                    else promote<CW, true, false>(taddr, rs, cs, acc);
+                } else {
+                    promote<CW, false, false>(taddr, rs, cs, acc);
                 }
             }
+            if constexpr (MAGIC) ptx::tmem_st_wait();
             ptx::tc_fence_before();
         }
         __syncwarp();
-        if (ptx::elect_one()) ptx::mbar_arrive(ptx::smem_u32(&sh->slot_free[slot]));
+        if (ptx::elect_one()) {
+            if constexpr (PAIR) {
+                ptx::mbar_arrive(ptx::smem_u32(&sh->scale_free[slot]));
+                ptx::mbar_arrive_cluster(ec.free_bar + 8u * slot);
+            } else {
+                ptx::mbar_arrive(ec.free_bar + 8u * slot);
+            }
+        }
+        __syncwarp();
         if (++slot == NSLOT) { slot = 0; sphase ^= 1u; }
     }
-    if (a.split > 1) {           // [column][lane of TMEM], one float of padding per column
+    if constexpr (!PAIR) {
+        if (a.split > 1) {           // [column][lane of TMEM], one float of padding per column
 #pragma unroll
-        for (int j = 0; j < CW; ++j)
-            partial[(c0 + j) * (BM + 1) + quarter * 32 + lane] = j & 1 ? acc[j / 2].y : acc[j / 2].x;
-        return true;
+            for (int j = 0; j < CW; ++j)
+                ec.partial[(ec.c0 + j) * (BM + 1) + quarter * 32 + lane] = j & 1 ? acc[j / 2].y : acc[j / 2].x;
+            return true;
+        }
     }
     if (active) {
-        if constexpr (SWAP) finish_columns<CW>(a.out, col0 + c0, row0 + quarter * 32 + lane, acc);
-        else finish_rows<CW, C::PATCH_COLS>(a.out, patch, lane, row0 + quarter * 32, col0 + c0, acc);
+        if constexpr (SWAP) finish_columns<CW>(a.out, col0 + ec.c0, row0 + quarter * 32 + lane, acc);
+        else finish_rows<CW, C::PATCH_COLS>(a.out, ec.patch, lane, row0 + quarter * 32, col0 + ec.c0, acc);
     }
     return true;
 }
@@ -420,17 +514,27 @@ uint32_t rr[2][LD];
 // The MMA issuer's loop.  GST: steps of 32 channels per group, 4 standing for any multiple of four (groups begin and end
 // with a stage), 0 for every other number.  Its instructions form one dependent chain: with the place of a step in its
 // group decided at run time a stage of four MMAs took 1270 cycles.
-template <int BN, bool SWAP, int GST>
+template <int BN, bool SWAP, bool PAIR, int GST>
 __device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tmem_base, const MmaArgs &a, const Range &rg,
                                       const WaitCtx &ctx, int first, int stride)
 {
-    using C = Cfg<BN, SWAP>;
+    using C = Cfg<BN, SWAP, PAIR>;
     constexpr uint32_t dhi = ptx::smem_desc_sw128_hi();
-    constexpr uint32_t idesc = ptx::idesc_i8(BM, BN);
+    constexpr uint32_t idesc = ptx::idesc_i8(PAIR ? 2 * BM : BM, BN);
+    constexpr bool MAGIC = kUseMagic<SWAP>;                              // sums are added to what the epilogue wrote
+    constexpr uint32_t FIRST = MAGIC ? 0u : 1u;                          // the epilogue has to have freed a slot first
     constexpr int PER = GST == 1 || GST == 2 ? 4 / GST : 1;              // groups per stage
     constexpr int CG = PER < C::CG_MAX ? PER : C::CG_MAX;                // pieces per chunk
     const uint32_t full0 = ptx::smem_u32(&sh->full[0]), empty0 = ptx::smem_u32(&sh->empty[0]);
     const uint32_t acc0 = ptx::smem_u32(&sh->acc_full[0]), free0 = ptx::smem_u32(&sh->slot_free[0]);
+    auto mma = [&](uint32_t d, uint32_t al, uint32_t bl, bool first_step) {
+        if constexpr (PAIR) ptx::umma_i8_pair(d, al, bl, dhi, idesc, MAGIC || !first_step);
+        else ptx::umma_i8_lo(d, al, bl, dhi, idesc, MAGIC || !first_step);
+    };
+    auto commit = [&](uint32_t bar) {
+        if constexpr (PAIR) ptx::umma_commit_pair(bar);
+        else ptx::umma_commit(bar);
+    };
     int stage = 0, slot = 0;
     uint32_t phase = 0, sphase = 0;
     for (int t = first; t < a.tiles; t += stride) {
@@ -438,34 +542,34 @@ __device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tm
         bool begins = true;                                              // the next step is the first of its piece
         for (int kb = rg.kb0; kb < rg.kb1; ++kb) {
             const int n = min(4, rg.s1 - 4 * kb);
-            if (!wait_warp(full0 + 8u * stage, phase, ctx, kWaitSmemFull)) return;
+            if (!wait<C>(full0 + 8u * stage, phase, ctx, kWaitSmemFull)) return;
             const uint32_t a_lo = tiles_lo + (uint32_t)(stage * (C::STAGE_BYTES >> 4));
             const uint32_t b_lo = a_lo + (uint32_t)(A_BYTES >> 4);
             if constexpr (GST == 4) {
-                if (begins && !wait_warp(free0 + 8u * slot, sphase ^ 1u, ctx, kWaitTmemEmpty)) return;
+                if (begins && !wait<C>(free0 + 8u * slot, sphase ^ FIRST, ctx, kWaitTmemEmpty)) return;
                 in_group += n;
-                const bool ends = in_group == a.gsteps || 4 * kb + n == rg.s1;
+                const bool ends = in_group == a.gsteps || in_group % PIECE == 0 || 4 * kb + n == rg.s1;
                 ptx::tc_fence_after();
                 if (ptx::elect_one()) {
                     const uint32_t d = tmem_base + (uint32_t)(slot * SLOT_COLS);
-                    ptx::umma_i8_lo(d, a_lo, b_lo, dhi, idesc, !begins);
-                    if (n > 1) ptx::umma_i8_lo<true>(d, a_lo + 2, b_lo + 2, dhi, idesc);
-                    if (n > 2) ptx::umma_i8_lo<true>(d, a_lo + 4, b_lo + 4, dhi, idesc);
-                    if (n > 3) ptx::umma_i8_lo<true>(d, a_lo + 6, b_lo + 6, dhi, idesc);
-                    ptx::umma_commit(empty0 + 8u * stage);
-                    if (ends) ptx::umma_commit(acc0 + 8u * slot);
+                    mma(d, a_lo, b_lo, begins);
+                    if (n > 1) mma(d, a_lo + 2, b_lo + 2, false);
+                    if (n > 2) mma(d, a_lo + 4, b_lo + 4, false);
+                    if (n > 3) mma(d, a_lo + 6, b_lo + 6, false);
+                    commit(empty0 + 8u * stage);
+                    if (ends) commit(acc0 + 8u * slot);
                 }
                 __syncwarp();
                 begins = ends;
+                if (in_group == a.gsteps) in_group = 0;
                 if (ends) {
-                    in_group = 0;
                     if (++slot == NSLOT) { slot = 0; sphase ^= 1u; }
                 }
             } else if constexpr (GST > 0) {
 #pragma unroll
                 for (int c = 0; c < 4; c += CG * GST) {                  // chunks of the stage
                     if (c < n) {
-                        if (!wait_warp(free0 + 8u * slot, sphase ^ 1u, ctx, kWaitTmemEmpty)) return;
+                        if (!wait<C>(free0 + 8u * slot, sphase ^ FIRST, ctx, kWaitTmemEmpty)) return;
                         ptx::tc_fence_after();
                         if (ptx::elect_one()) {
                             const uint32_t d = tmem_base + (uint32_t)(slot * SLOT_COLS);
@@ -473,38 +577,37 @@ __device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tm
                             for (int s = c; s < c + CG * GST; ++s)
                                 if (s < n) {
                                     const uint32_t dj = d + (uint32_t)((s - c) / GST * BN), off = 2u * s;
-                                    if (s % GST) ptx::umma_i8_lo<true>(dj, a_lo + off, b_lo + off, dhi, idesc);
-                                    else ptx::umma_i8_lo<false>(dj, a_lo + off, b_lo + off, dhi, idesc);
+                                    mma(dj, a_lo + off, b_lo + off, s % GST == 0);
                                 }
-                            ptx::umma_commit(acc0 + 8u * slot);
+                            commit(acc0 + 8u * slot);
                         }
                         __syncwarp();
                         if (++slot == NSLOT) { slot = 0; sphase ^= 1u; }
                     }
                 }
-                if (ptx::elect_one()) ptx::umma_commit(empty0 + 8u * stage);
+                if (ptx::elect_one()) commit(empty0 + 8u * stage);
                 __syncwarp();
             } else {
                 ptx::tc_fence_after();
                 for (int s = 0; s < n; ++s) {
                     if (begins) {
-                        if (!wait_warp(free0 + 8u * slot, sphase ^ 1u, ctx, kWaitTmemEmpty)) return;
+                        if (!wait<C>(free0 + 8u * slot, sphase ^ FIRST, ctx, kWaitTmemEmpty)) return;
                         ptx::tc_fence_after();
                     }
-                    const bool ends = ++in_group == a.gsteps || 4 * kb + s + 1 == rg.s1;
+                    const bool ends = ++in_group == a.gsteps || in_group % PIECE == 0 || 4 * kb + s + 1 == rg.s1;
                     if (ptx::elect_one()) {
                         const uint32_t d = tmem_base + (uint32_t)(slot * SLOT_COLS);
-                        ptx::umma_i8_lo(d, a_lo + 2 * s, b_lo + 2 * s, dhi, idesc, !begins);
-                        if (ends) ptx::umma_commit(acc0 + 8u * slot);
+                        mma(d, a_lo + 2 * s, b_lo + 2 * s, begins);
+                        if (ends) commit(acc0 + 8u * slot);
                     }
                     __syncwarp();
                     begins = ends;
+                    if (in_group == a.gsteps) in_group = 0;
                     if (ends) {
-                        in_group = 0;
                         if (++slot == NSLOT) { slot = 0; sphase ^= 1u; }
                     }
                 }
-                if (ptx::elect_one()) ptx::umma_commit(empty0 + 8u * stage);
+                if (ptx::elect_one()) commit(empty0 + 8u * stage);
                 __syncwarp();
             }
             if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
@@ -512,19 +615,22 @@ __device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tm
     }
 }
 
-template <int BN, bool SWAP>
+template <int BN, bool SWAP, bool PAIR>
 __global__ void __launch_bounds__(THREADS, 1)
 linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, MmaArgs a)
 {
-    using C = Cfg<BN, SWAP>;
+    using C = Cfg<BN, SWAP, PAIR>;
+    constexpr bool MAGIC = kUseMagic<SWAP>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *tiles = ptx::align_smem<1024>(smem_raw);
     float *patches = reinterpret_cast<float *>(tiles + (size_t)C::STAGES * C::STAGE_BYTES);
     float *scales = patches + EPI_WARPS * (C::PATCH_BYTES / 4);
     Shared *sh = reinterpret_cast<Shared *>(scales + (size_t)NSLOT * C::SLOT_SCALE_FLOATS);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = (int)blockIdx.x % a.split, first = (int)blockIdx.x / a.split, stride = (int)gridDim.x / a.split;
-    const Range rg = range_of(a, rank);
+    const int ctas = PAIR ? 2 : a.split;                                   // of a cluster
+    const int rank = (int)blockIdx.x % ctas, first = (int)blockIdx.x / ctas, stride = (int)gridDim.x / ctas;
+    const Range rg = range_of(a, PAIR ? 0 : rank);
+    const int row_block = PAIR ? 2 * BM : BM, row_off = PAIR ? rank * BM : 0;
     const WaitCtx ctx{&sh->abort, a.status, a.wait_cycles};
 
     if (threadIdx.x == 0) {
@@ -534,20 +640,28 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         }
         for (int s = 0; s < NSLOT; ++s) {
             ptx::mbar_init(ptx::smem_u32(&sh->acc_full[s]), 2);       // MMAs, scales
-            ptx::mbar_init(ptx::smem_u32(&sh->slot_free[s]), EPI_WARPS);
+            ptx::mbar_init(ptx::smem_u32(&sh->slot_free[s]), (PAIR ? 2 : 1) * EPI_WARPS);
+            ptx::mbar_init(ptx::smem_u32(&sh->scale_free[s]), EPI_WARPS);
         }
         ptx::mbar_init(ptx::smem_u32(&sh->mma_done), 1);
         sh->abort = 0;
         ptx::fence_mbar_init();
     }
     if (warp == 1) {
-        ptx::tmem_alloc(ptx::smem_u32(&sh->tmem_base), TMEM_COLS);
-        ptx::tmem_relinquish();
+        if constexpr (PAIR) {
+            ptx::tmem_alloc_pair(ptx::smem_u32(&sh->tmem_base), TMEM_COLS);
+            ptx::tmem_relinquish_pair();
+        } else {
+            ptx::tmem_alloc(ptx::smem_u32(&sh->tmem_base), TMEM_COLS);
+            ptx::tmem_relinquish();
+        }
     }
     ptx::tc_fence_before();
     __syncthreads();
+    if constexpr (PAIR) ptx::cluster_sync();          // the other CTA's barriers are initialised, its tensor memory is allocated
     ptx::tc_fence_after();
     const uint32_t tmem_base = sh->tmem_base;
+    const bool rank_issues = !PAIR || rank == 0;
     if (warp == 0 && ptx::elect_one()) {
         ptx::prefetch_tmap(&tmA);
         ptx::prefetch_tmap(&tmB);
@@ -556,6 +670,8 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
 
+    if (warp < FIRST_EPI_WARP) {
+    if constexpr (C::MOVE_REGS) ptx::fewer_registers<40>();
     if (warp == 0) {
         // ---------------- TMA producer ----------------
         int stage = 0;
@@ -565,14 +681,21 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         for (int t = first; t < a.tiles && ok; t += stride) {
             const int mt = t % a.MT, nt = t / a.MT;
             for (int kb = rg.kb0; kb < rg.kb1; ++kb) {
-                ok = wait_warp(ptx::smem_u32(&sh->empty[stage]), phase ^ 1u, ctx, kWaitSmemEmpty);
+                ok = wait<C>(ptx::smem_u32(&sh->empty[stage]), phase ^ 1u, ctx, kWaitSmemEmpty);
                 if (!ok) break;
                 if (ptx::elect_one() && !(blockIdx.x == 0 && issued == a.debug_skip_stage)) {
                     const uint32_t bar = ptx::smem_u32(&sh->full[stage]);
                     const uint32_t dst = ptx::smem_u32(tiles + (size_t)stage * C::STAGE_BYTES);
-                    ptx::mbar_arrive_expect_tx(bar, C::STAGE_BYTES);
-                    ptx::tma_load_2d(dst, &tmA, bar, kb * BK, mt * BM);
-                    ptx::tma_load_2d(dst + A_BYTES, &tmB, bar, kb * BK, nt * BN);
+                    if constexpr (PAIR) {      // the leader's barrier counts both CTAs' bytes
+                        const uint32_t lead = ptx::map_rank(bar, 0);
+                        if (rank == 0) ptx::mbar_arrive_expect_tx(bar, 2 * C::STAGE_BYTES);
+                        ptx::tma_load_2d_pair(dst, &tmA, lead, kb * BK, mt * row_block + row_off);
+                        ptx::tma_load_2d_pair(dst + A_BYTES, &tmB, lead, kb * BK, nt * BN + rank * C::B_ROWS);
+                    } else {
+                        ptx::mbar_arrive_expect_tx(bar, C::STAGE_BYTES);
+                        ptx::tma_load_2d(dst, &tmA, bar, kb * BK, mt * BM);
+                        ptx::tma_load_2d(dst + A_BYTES, &tmB, bar, kb * BK, nt * BN);
+                    }
                 }
                 __syncwarp();
                 ++issued;
@@ -588,24 +711,27 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                 drain(ptx::smem_u32(&sh->full[s]), ph);
             }
         }
-    } else if (warp == 1) {
+    } else if (warp == 1 && rank_issues) {
         // ---------------- MMA issuer ----------------
         const uint32_t tiles_lo = ptx::smem_desc_sw128_lo(ptx::smem_u32(tiles));
-        if (a.gsteps % 4 == 0 || a.gsteps >= a.steps) issue<BN, SWAP, 4>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
-        else if (a.gsteps == 2) issue<BN, SWAP, 2>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
-        else if (a.gsteps == 1) issue<BN, SWAP, 1>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
-        else issue<BN, SWAP, 0>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
+        if (a.gsteps % 4 == 0 || a.gsteps >= a.steps) issue<BN, SWAP, PAIR, 4>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
+        else if (a.gsteps == 2) issue<BN, SWAP, PAIR, 2>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
+        else if (a.gsteps == 1) issue<BN, SWAP, PAIR, 1>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
+        else issue<BN, SWAP, PAIR, 0>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
     } else if (warp == 2) {
         // ---------------- scale loader ----------------
+        const uint32_t scale_bar = ptx::smem_u32(PAIR ? &sh->scale_free[0] : &sh->slot_free[0]);
         int slot = 0;
         uint32_t sphase = 0;
         long long issued = 0;
         bool ok = true;
         for (int t = first; t < a.tiles && ok; t += stride) {
             const int mt = t % a.MT, nt = t / a.MT;
+            // the second CTA of a pair may have no rows: it then reads scales that it does not use
+            const long long row0 = min((long long)mt * row_block + row_off, a.row_pitch - BM);
             for (int q0 = 0; q0 < rg.np; q0 += a.cg) {
                 const int n = min(a.cg, rg.np - q0);
-                ok = wait_warp(ptx::smem_u32(&sh->slot_free[slot]), sphase ^ 1u, ctx, kWaitScaleEmpty);
+                ok = wait<C>(scale_bar + 8u * slot, sphase ^ (MAGIC ? 0u : 1u), ctx, kWaitScaleEmpty);
                 if (!ok) break;
                 const uint32_t bar = ptx::smem_u32(&sh->acc_full[slot]);
                 const uint32_t dst = ptx::smem_u32(scales + (size_t)slot * C::SLOT_SCALE_FLOATS);
@@ -613,9 +739,9 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                 __syncwarp();
                 if (lane < 8 && (lane & 3) < n) {      // lane j: row scales of piece j, lane 4 + j: column scales
                     const int j = lane & 3;
-                    const long long g = rg.g0 + q0 + j;
+                    const long long g = (rg.p0 + q0 + j) / a.ppg;
                     const uint32_t d = dst + (uint32_t)(j * C::GROUP_SCALE_FLOATS * 4);
-                    if (lane < 4) ptx::bulk_load(d, a.row_scale + g * a.row_pitch + mt * BM, BM * 4, bar);
+                    if (lane < 4) ptx::bulk_load(d, a.row_scale + g * a.row_pitch + row0, BM * 4, bar);
                     else ptx::bulk_load(d + BM * 4, a.col_scale + g * a.col_pitch + nt * BN, BN * 4, bar);
                 }
                 __syncwarp();
@@ -632,23 +758,53 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                 drain(ptx::smem_u32(&sh->acc_full[s]), ph);
             }
         }
-    } else if (warp >= FIRST_EPI_WARP) {
+    }
+    } else {
         // ---------------- epilogue ----------------
+        if constexpr (C::MOVE_REGS) ptx::more_registers<232>();
         const int e = warp - FIRST_EPI_WARP, quarter = warp & 3;
         int slot = 0;
         uint32_t sphase = 0;
-        const uint32_t tmem = tmem_base + ((uint32_t)(quarter * 32) << 16);
+        EpiCtx ec;
+        ec.c0 = (e >> 2) * (BN / 2);
+        ec.tmem = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)ec.c0;
+        ec.scales = scales;
+        ec.patch = patches + e * (C::PATCH_BYTES / 4);
+        ec.partial = reinterpret_cast<float *>(tiles);
+        ec.free_bar = ptx::smem_u32(&sh->slot_free[0]);
+        if constexpr (PAIR) ec.free_bar = ptx::map_rank(ec.free_bar, 0);
+        ec.quarter = quarter;
+        ec.lane = lane;
+        if constexpr (MAGIC) {
+            // the slots start from the pattern: this warp's lanes and columns of every piece
+            uint32_t pattern[8];
+            for (int i = 0; i < 8; ++i) pattern[i] = kMagicBits;
+            for (int s = 0; s < NSLOT; ++s)
+                for (int c = 0; c < C::CG_MAX * BN; c += BN)
+                    for (int i = 0; i < BN / 2; i += 8) ptx::tmem_st_x8(ec.tmem + (uint32_t)(s * SLOT_COLS + c + i), pattern);
+            ptx::tmem_st_wait();
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (ptx::elect_one()) {
+                for (int s = 0; s < NSLOT; ++s) {
+                    if constexpr (PAIR) {
+                        ptx::mbar_arrive(ptx::smem_u32(&sh->scale_free[s]));
+                        ptx::mbar_arrive_cluster(ec.free_bar + 8u * s);
+                    } else {
+                        ptx::mbar_arrive(ec.free_bar + 8u * s);
+                    }
+                }
+            }
+            __syncwarp();
+        }
         for (int t = first; t < a.tiles; t += stride) {
             const int mt = t % a.MT, nt = t / a.MT;
-            if (!epilogue_tile<BN, SWAP>(sh, a, ctx, tmem, scales, patches + e * (C::PATCH_BYTES / 4),
-                                         reinterpret_cast<float *>(tiles), e >> 2, quarter, lane, mt * BM, nt * BN, rg,
-                                         slot, sphase))
-                break;
+            if (!epilogue_tile<BN, SWAP, PAIR>(sh, a, ctx, ec, mt * row_block + row_off, nt * BN, rg, slot, sphase)) break;
         }
     }
 
     __syncwarp();
-    if (a.split > 1) {
+    if (!PAIR && a.split > 1) {
         // one tile per cluster: the partial sums are complete, each CTA adds up its share of the columns in rank order
         ptx::cluster_sync();
         const int share = BN / a.split;             // even: at least 2
@@ -678,46 +834,58 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     }
     ptx::tc_fence_before();
     __syncthreads();
-    if (warp == 1) {
-        if (sh->abort) {
-            if (ptx::elect_one()) ptx::umma_commit(ptx::smem_u32(&sh->mma_done));
-            __syncwarp();
-            drain(ptx::smem_u32(&sh->mma_done), 0);
+    if (warp == 1 && sh->abort) {       // MMAs may still be in flight; with PAIR the other CTA's copies and MMAs too
+        if (rank_issues && ptx::elect_one()) {
+            if constexpr (PAIR) ptx::umma_commit_pair(ptx::smem_u32(&sh->mma_done));
+            else ptx::umma_commit(ptx::smem_u32(&sh->mma_done));
         }
+        __syncwarp();
+        drain(ptx::smem_u32(&sh->mma_done), 0);
+    }
+    if constexpr (PAIR) ptx::cluster_sync();        // nobody leaves while the pair's MMAs read or write its memory
+    if (warp == 1) {
         ptx::tc_fence_after();
-        ptx::tmem_dealloc(tmem_base, TMEM_COLS);
+        if constexpr (PAIR) ptx::tmem_dealloc_pair(tmem_base, TMEM_COLS);
+        else ptx::tmem_dealloc(tmem_base, TMEM_COLS);
     }
 }
 
-// How a call is laid out: orientation, columns per tile, CTAs per tile.
-struct Shape { bool swap; int bn, split; };
+// How a call is laid out: orientation (1: rows of x on the lanes, 2: outputs, 3: pairs of CTAs with rows of x), columns
+// per tile, CTAs that share a tile's channels.
+struct Shape { int orient, bn, split; };
+
+bool known_shape(const Shape &s)
+{
+    if (s.orient == 1) return s.bn == 64 || s.bn == 128;
+    if (s.orient == 2) return s.bn == 16 || s.bn == 32 || s.bn == 64;
+    return s.orient == 3 && s.split == 1 && (s.bn == 128 || s.bn == 256);
+}
 
 Shape choose(const wfq_linear &l, int rows)
 {
-    if (l.debug_shape) {
-        const int v = l.debug_shape;
-        return Shape{v / 1000 % 10 == 2, v % 1000, v / 10000};
-    }
+    if (l.debug_shape) return Shape{l.debug_shape / 1000 % 10, l.debug_shape % 1000, l.debug_shape / 10000};
     const int KB = (l.Cp / 32 + 3) / 4;
-    Shape best{false, 64, 1};
+    Shape best{1, 64, 1};
     double best_cost = 1e300;
-    for (int swap = 0; swap < 2; ++swap)
-        for (int bn : {256, 128, 64, 32, 16}) {
-            if (swap ? bn > 64 : bn < 64) continue;
-            const int r = swap ? l.Kz : rows, c = swap ? rows : l.Kz;
-            const double tiles = (double)((r + BM - 1) / BM) * ((c + bn - 1) / bn);
+    for (int orient = 1; orient <= 3; ++orient)
+        for (int bn : {256, 128, 64, 32, 16})
             for (int split : {1, 2, 4, 8}) {
+                const Shape sp{orient, bn, split};
+                if (!known_shape(sp)) continue;
+                const int lanes = orient == 3 ? 2 * BM : BM, per_tile = orient == 3 ? 2 : split;
+                const int r = orient == 2 ? l.Kz : rows, c = orient == 2 ? rows : l.Kz;
+                const double tiles = (double)((r + lanes - 1) / lanes) * ((c + bn - 1) / bn);
                 if (split > 1 && (tiles * split > l.sm_count || KB < 2 * split)) continue;
-                const double per_group = BM * bn / 45.0 + 200.0;
-                const double groups = l.gs < 128 ? 128.0 / l.gs : 128.0 / (l.gs < 1024 ? l.gs : 1024);
-                double per_stage = groups * per_group;
-                if (per_stage < (BM + bn) * 128 / 45.0) per_stage = (BM + bn) * 128 / 45.0;
-                const double waves = (double)(long long)((tiles * split + l.sm_count - 1) / l.sm_count);
-                const double cost = waves * (((KB + split - 1) / split) * per_stage + BM * bn / 8.0) +
-                                    (split > 1 ? 2000.0 : 0.0);
-                if (cost < best_cost) { best_cost = cost; best = Shape{swap != 0, bn, split}; }
+                const double per_piece = BM * bn / 45.0 + 200.0;
+                const double pieces = l.gs < 256 ? 128.0 / l.gs : 0.5;
+                double per_stage = pieces * per_piece;
+                const double bytes = (BM + (orient == 3 ? bn / 2 : bn)) * 128.0;
+                if (per_stage < bytes / 50.0) per_stage = bytes / 50.0;
+                const int at_once = l.sm_count / per_tile;
+                const double waves = (double)(long long)((tiles + at_once - 1) / at_once);
+                const double cost = waves * (((KB + split - 1) / split) * per_stage + BM * bn / 8.0) + (split > 1 ? 2000.0 : 0.0);
+                if (cost < best_cost) { best_cost = cost; best = sp; }
             }
-        }
     return best;
 }
 
@@ -729,26 +897,26 @@ bool encode_codes(CUtensorMap *map, const int8_t *codes, int Cp, int rows, int b
     return encode_tmap(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, codes, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <int BN, bool SWAP>
+template <int BN, bool SWAP, bool PAIR>
 cudaError_t setup_variant()
 {
-    return cudaFuncSetAttribute(linear_mma_kernel<BN, SWAP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                (int)Cfg<BN, SWAP>::SMEM_BYTES);
+    return cudaFuncSetAttribute(linear_mma_kernel<BN, SWAP, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                (int)Cfg<BN, SWAP, PAIR>::SMEM_BYTES);
 }
 
-template <int BN, bool SWAP>
+template <int BN, bool SWAP, bool PAIR>
 cudaError_t launch_variant(const wfq_linear &l, MmaArgs &a, int grid, const int8_t *xq, int rows, cudaStream_t stream,
                            bool pdl)
 {
     a.cg = 1;
-    if (BK % l.gs == 0) a.cg = BK / l.gs < Cfg<BN, SWAP>::CG_MAX ? BK / l.gs : Cfg<BN, SWAP>::CG_MAX;
+    if (BK % l.gs == 0) a.cg = BK / l.gs < Cfg<BN, SWAP, PAIR>::CG_MAX ? BK / l.gs : Cfg<BN, SWAP, PAIR>::CG_MAX;
     CUtensorMap tx, tw;
-    if (!encode_codes(&tx, xq, l.Cp, rows, SWAP ? BN : BM) || !encode_codes(&tw, l.Wq, l.Cp, l.Kz, SWAP ? BM : BN))
+    if (!encode_codes(&tx, xq, l.Cp, rows, SWAP ? BN : BM) || !encode_codes(&tw, l.Wq, l.Cp, l.Kz, SWAP ? BM : Cfg<BN, SWAP, PAIR>::B_ROWS))
         return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = Cfg<BN, SWAP>::SMEM_BYTES;
+    cfg.dynamicSmemBytes = Cfg<BN, SWAP, PAIR>::SMEM_BYTES;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     int n = 0;
@@ -756,15 +924,15 @@ cudaError_t launch_variant(const wfq_linear &l, MmaArgs &a, int grid, const int8
         attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         attr[n++].val.programmaticStreamSerializationAllowed = 1;
     }
-    if (a.split > 1) {
+    if (PAIR || a.split > 1) {
         attr[n].id = cudaLaunchAttributeClusterDimension;
-        attr[n].val.clusterDim.x = (unsigned)a.split;
+        attr[n].val.clusterDim.x = PAIR ? 2u : (unsigned)a.split;
         attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
         ++n;
     }
     cfg.attrs = attr;
     cfg.numAttrs = (unsigned)n;
-    return cudaLaunchKernelEx(&cfg, linear_mma_kernel<BN, SWAP>, SWAP ? tw : tx, SWAP ? tx : tw, a);
+    return cudaLaunchKernelEx(&cfg, linear_mma_kernel<BN, SWAP, PAIR>, SWAP ? tw : tx, SWAP ? tx : tw, a);
 }
 
 cudaError_t launch_product(wfq_linear &l, const int8_t *xq, const float *sx, int rows, const OutArgs &out,
@@ -773,31 +941,37 @@ cudaError_t launch_product(wfq_linear &l, const int8_t *xq, const float *sx, int
     const Shape sp = choose(l, rows);
     MmaArgs a;
     const long long sx_pitch = (rows + 127LL) / 128 * 128;
-    a.row_scale = sp.swap ? l.sW : sx;
-    a.col_scale = sp.swap ? sx : l.sW;
-    a.row_pitch = sp.swap ? l.Kp : sx_pitch;
-    a.col_pitch = sp.swap ? sx_pitch : l.Kp;
-    a.rows = sp.swap ? l.Kz : rows;
-    a.cols = sp.swap ? rows : l.Kz;
-    a.MT = (a.rows + BM - 1) / BM;
+    const bool swap = sp.orient == 2, pair = sp.orient == 3;
+    a.row_scale = swap ? l.sW : sx;
+    a.col_scale = swap ? sx : l.sW;
+    a.row_pitch = swap ? l.Kp : sx_pitch;
+    a.col_pitch = swap ? sx_pitch : l.Kp;
+    a.rows = swap ? l.Kz : rows;
+    a.cols = swap ? rows : l.Kz;
+    a.MT = (int)((a.rows + (pair ? 2LL : 1LL) * BM - 1) / (pair ? 2 * BM : BM));
     a.tiles = a.MT * ((a.cols + sp.bn - 1) / sp.bn);
     a.split = sp.split;
     a.steps = l.Cp / UK;
     a.gsteps = l.gs / UK;
+    a.ppg = (a.gsteps + PIECE - 1) / PIECE;
     a.status = l.status;
     a.wait_cycles = l.wait_cycles;
     a.debug_skip_stage = l.debug_skip_stage;
     a.early = 0;
     a.out = out;
-    const int grid = sp.split > 1 ? a.tiles * sp.split : a.tiles < l.sm_count ? a.tiles : l.sm_count;
-    if (sp.swap) {
-        if (sp.bn == 16) return launch_variant<16, true>(l, a, grid, xq, rows, stream, pdl);
-        if (sp.bn == 32) return launch_variant<32, true>(l, a, grid, xq, rows, stream, pdl);
-        return launch_variant<64, true>(l, a, grid, xq, rows, stream, pdl);
+    const int at_once = pair ? l.sm_count / 2 : l.sm_count;
+    const int grid = sp.split > 1 ? a.tiles * sp.split : (a.tiles < at_once ? a.tiles : at_once) * (pair ? 2 : 1);
+    if (swap) {
+        if (sp.bn == 16) return launch_variant<16, true, false>(l, a, grid, xq, rows, stream, pdl);
+        if (sp.bn == 32) return launch_variant<32, true, false>(l, a, grid, xq, rows, stream, pdl);
+        return launch_variant<64, true, false>(l, a, grid, xq, rows, stream, pdl);
     }
-    if (sp.bn == 64) return launch_variant<64, false>(l, a, grid, xq, rows, stream, pdl);
-    if (sp.bn == 128) return launch_variant<128, false>(l, a, grid, xq, rows, stream, pdl);
-    return launch_variant<256, false>(l, a, grid, xq, rows, stream, pdl);
+    if (pair) {
+        if (sp.bn == 128) return launch_variant<128, false, true>(l, a, grid, xq, rows, stream, pdl);
+        return launch_variant<256, false, true>(l, a, grid, xq, rows, stream, pdl);
+    }
+    if (sp.bn == 64) return launch_variant<64, false, false>(l, a, grid, xq, rows, stream, pdl);
+    return launch_variant<128, false, false>(l, a, grid, xq, rows, stream, pdl);
 }
 
 bool known(wfq_dtype_t t) { return t == WFQ_F32 || t == WFQ_F16 || t == WFQ_BF16; }
@@ -817,12 +991,13 @@ wfq_status_t bind(wfq_linear *l)
     if (s != WFQ_OK) return s;
     if (l->device == dev) return WFQ_OK;
     if (l->device >= 0) return WFQ_ERR_INVALID_ARG;
-    cudaError_t e = setup_variant<16, true>();
-    if (e == cudaSuccess) e = setup_variant<32, true>();
-    if (e == cudaSuccess) e = setup_variant<64, true>();
-    if (e == cudaSuccess) e = setup_variant<64, false>();
-    if (e == cudaSuccess) e = setup_variant<128, false>();
-    if (e == cudaSuccess) e = setup_variant<256, false>();
+    cudaError_t e = setup_variant<16, true, false>();
+    if (e == cudaSuccess) e = setup_variant<32, true, false>();
+    if (e == cudaSuccess) e = setup_variant<64, true, false>();
+    if (e == cudaSuccess) e = setup_variant<64, false, false>();
+    if (e == cudaSuccess) e = setup_variant<128, false, false>();
+    if (e == cudaSuccess) e = setup_variant<128, false, true>();
+    if (e == cudaSuccess) e = setup_variant<256, false, true>();
     if (e != cudaSuccess) return WFQ_ERR_CUDA;
     l->device = dev;
     l->sm_count = sms;
@@ -1013,12 +1188,10 @@ wfq_status_t wfq_linear_set_debug_option(wfq_linear_t *l, wfq_debug_option_t opt
             l->debug_skip_stage = (int)value;
             return WFQ_OK;
         case WFQ_DEBUG_GEMM_SHAPE: {
-            const long long bn = value % 1000, orient = value / 1000 % 10, split = value / 10000;
-            const bool normal = orient == 1 && (bn == 64 || bn == 128 || bn == 256);
-            const bool swapped = orient == 2 && (bn == 16 || bn == 32 || bn == 64);
-            const bool parts = split == 1 || split == 2 || split == 4 || split == 8;
+            const Shape sp{(int)(value / 1000 % 10), (int)(value % 1000), (int)(value / 10000)};
+            const bool parts = sp.split == 1 || sp.split == 2 || sp.split == 4 || sp.split == 8;
             // every CTA of a tile needs at least 128 channels
-            if (value != 0 && (value < 0 || !parts || !(normal || swapped) || (l->Cp + 127) / 128 < split))
+            if (value != 0 && (value < 0 || value > 99999 || !parts || !known_shape(sp) || (l->Cp + 127) / 128 < sp.split))
                 return WFQ_ERR_INVALID_ARG;
             l->debug_shape = (int)value;
             return WFQ_OK;

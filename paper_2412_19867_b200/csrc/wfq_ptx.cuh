@@ -412,6 +412,57 @@ __device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[8])
                  :: "memory");
 }
 
+// ---- pairs of CTAs (cta_group::2) ----------------------------------------------------
+// The even CTA of a cluster of two issues MMAs of 256 rows: each CTA holds its 128 rows of A, half of B's rows and, in its
+// tensor memory, its 128 rows of D; the operands lie at the same shared-memory addresses in both.
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t smem_dst, uint32_t ncols)
+{
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(ncols) : "memory");
+}
+__device__ __forceinline__ void tmem_relinquish_pair()
+{
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t ncols)
+{
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+}
+__device__ __forceinline__ void umma_i8_pair(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t desc_hi,
+                                             uint32_t idesc, bool accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .b64 da, db;\n\t.reg .pred p;\n\t"
+        "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::i8 [%0], da, db, %4, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(desc_hi), "r"(idesc), "r"((uint32_t)accumulate));
+}
+// Arrive on `bar` (the same offset in both CTAs) once all MMAs issued so far by this thread have completed.
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar)
+{
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+        ::"r"(bar), "h"((uint16_t)3)
+        : "memory");
+}
+// 2-D tiled load into this CTA's shared memory, its bytes counted on a barrier of either CTA (a cluster address).
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%3, %4}], [%2];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1)
+        : "memory");
+}
+// Arrive on a barrier of any CTA of the cluster (a cluster address).
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// Registers of a warpgroup: less for the roles that move data, more for those that hold sums.
+template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+
 // ---- descriptors --------------------------------------------------------------------
 // Shared-memory matrix descriptor for a K-major operand tile stored as rows of 128
 // bytes with the 128-byte swizzle (8-row x 128-byte atoms, 1024 bytes apart):
@@ -462,10 +513,10 @@ struct WaitCtx {
     long long limit;        // clock cycles
 };
 
-// The waiting loop is kept out of line so that the role loops stay short.  The bare
+// The waiting loop.  The bare
 // try_wait suspends the thread in hardware for up to a millisecond; clock and abort flag
 // are looked at every 64 tries.
-static __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, const WaitCtx &ctx, int where)
+static __device__ __forceinline__ bool wait_loop(uint32_t bar, uint32_t parity, const WaitCtx &ctx, int where)
 {
     long long t0 = 0;
 #pragma unroll 1
@@ -486,6 +537,17 @@ static __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, con
             }
         }
     }
+}
+// The same kept out of line, so that the role loops stay short.
+static __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, const WaitCtx &ctx, int where)
+{
+    return wait_loop(bar, parity, ctx, where);
+}
+// wait_warp() below without a call, for kernels whose warpgroups move registers between them (no call is possible there).
+__device__ __forceinline__ bool wait_warp_inline(uint32_t bar, uint32_t parity, const WaitCtx &ctx, int where)
+{
+    if (__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity))) return true;
+    return __all_sync(0xffffffffu, wait_loop(bar, parity, ctx, where));
 }
 // The wait of a whole converged warp, with one answer for all of its lanes: a warp whose lanes gave up one by one would
 // leave some of them behind in an instruction that needs the others (tcgen05.ld, elect.sync) and has no limit.  The vote
