@@ -57,6 +57,7 @@ constexpr int TMEM_COLS = NSLOT * SLOT_COLS;
 constexpr int A_BYTES = BM * BK;
 constexpr int EPI_WARPS = 8;
 constexpr int FIRST_EPI_WARP = 4;
+constexpr int PATCH_PITCH = 40;                                  // floats; 32 columns of z on their way out
 constexpr int THREADS = 32 * (FIRST_EPI_WARP + EPI_WARPS);
 
 struct Shared {
@@ -74,8 +75,7 @@ struct Cfg {
     static constexpr int B_ROWS = PAIR ? BN / 2 : BN;             // of the columns' operand in this CTA
     static constexpr int STAGE_BYTES = A_BYTES + B_ROWS * BK;
     static constexpr int STAGES = STAGE_BYTES > 24 * 1024 ? 5 : STAGE_BYTES > 20 * 1024 ? (SWAP ? 8 : 7) : 10;
-    static constexpr int PATCH_COLS = 32;                         // columns of z on their way out at a time
-    static constexpr int PATCH_BYTES = SWAP ? 0 : 32 * (PATCH_COLS + 4) * 4;      // of one epilogue warp
+    static constexpr int PATCH_BYTES = SWAP ? 0 : 32 * PATCH_PITCH * 4;           // of one epilogue warp
     static constexpr int CG_MAX = SLOT_COLS / BN < 4 ? SLOT_COLS / BN : 4;        // pieces per chunk at most
     static constexpr int GROUP_SCALE_FLOATS = BM + BN;
     static constexpr int SLOT_SCALE_FLOATS = CG_MAX * GROUP_SCALE_FLOATS;
@@ -267,17 +267,134 @@ __device__ __forceinline__ void activate_all(float (&z)[N], int act)
     }
 }
 
+// Sums in tensor memory start from the bit pattern of 1.5 * 2^23 instead of zero (MAGIC): read as a float, pattern + sum is
+// 1.5 * 2^23 + sum exactly for |sum| < 2^22, and 127 * 127 * 256 is below that.  The conversion and the product with the row
+// scale are then one multiply-add, f * rs - 1.5 * 2^23 * rs, which is sum * rs rounded once where the second product is
+// exact: the row scale is rounded to 22 bits for that (2^-23 of it at most).  The epilogue writes the pattern back behind
+// its reads.  Against conversions (64 a clock and SM) and two products it halves the issue slots per sum.
+constexpr uint32_t kMagicBits = 0x4b400000u;
+constexpr float kMagic = 12582912.f;
+// With SWAP (few rows of x, bound by the weights' bytes) sums are converted.
+template <bool SWAP> constexpr bool kUseMagic = !SWAP;
+
+__device__ __forceinline__ float round22(float s)
+{
+    const uint32_t u = __float_as_uint(s);
+    return s < 3e38f ? __uint_as_float((u + 1 + ((u >> 2) & 1)) & ~3u) : s;      // to nearest even; scales are not negative
+}
+
+// The sums of an epilogue warp, 32 rows of TMEM lanes x CW columns.  Where there are many columns (!SWAP) a thread has four
+// rows, lane / 4 + 8 q, and every fourth pair of columns, 8 j + 2 (lane % 4): a column scale is then read from shared
+// memory by four threads instead of by all 32.  With a row per thread the reads return CW floats to every lane, 1024 cycles
+// of the SM's 128 bytes a clock for a piece of 128 x 256, which bounded the kernel whatever the arithmetic
+// (4096 channels in groups of 128, 1050 cycles a piece of 128 x 128).  With SWAP (few columns) a thread has one row.
+template <int CW, bool SWAP> struct Sums;
+template <int CW> struct Sums<CW, false> {
+    float2 v[4][CW / 8];         // [q][j]
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int j = 0; j < CW / 8; ++j) v[q][j] = make_float2(0.f, 0.f);
+    }
+};
+template <int CW> struct Sums<CW, true> {
+    float2 v[CW / 2];
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int j = 0; j < CW / 2; ++j) v[j] = make_float2(0.f, 0.f);
+    }
+};
+
+// One piece, 32 columns at a time, 16 lanes after the other, with the next load on its way.  `rs`: scales of the thread's
+// rows; `cs`: the warp's column scales, from the thread's first column on.  BIG: row scales whose product with 1.5 * 2^23
+// could overflow.
+template <int CW, bool MAGIC, bool BIG>
+__device__ __forceinline__ void promote(uint32_t taddr, const float (&rs)[4], const float *cs, const uint32_t (&pattern)[8],
+                                        Sums<CW, false> &sums)
+{
+    float off[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) off[q] = -kMagic * rs[q];
+    uint32_t rr[2][16];
+    auto fetch = [&](int b) {      // block b: columns 32 (b / 2) on, lanes 16 (b % 2) on
+        ptx::tmem_ld_16x256b_x4(taddr + (uint32_t)(b / 2 * 32) + ((uint32_t)(b % 2 * 16) << 16), rr[b & 1]);
+    };
+    fetch(0);
+#pragma unroll
+    for (int b = 0; b < CW / 16; ++b) {
+        uint32_t (&r)[16] = rr[b & 1];
+        ptx::tmem_ld_wait(r);
+        if (b + 1 < CW / 16) fetch(b + 1);
+        if constexpr (MAGIC) {
+            if (b % 2) {           // all 32 lanes of these columns have been read
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) ptx::tmem_st_x8(taddr + (uint32_t)(b / 2 * 32 + i), pattern);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 c = *reinterpret_cast<const float2 *>(cs + b / 2 * 32 + 8 * j);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int q = b % 2 * 2 + h;
+                const uint32_t r0 = r[4 * j + 2 * h], r1 = r[4 * j + 2 * h + 1];
+                const float2 rs2 = make_float2(rs[q], rs[q]);
+                float2 f;
+                if constexpr (MAGIC) {
+                    f = make_float2(__uint_as_float(r0), __uint_as_float(r1));
+                    if constexpr (BIG) f = __fmul2_rn(__fadd2_rn(f, make_float2(-kMagic, -kMagic)), rs2);
+                    else f = __ffma2_rn(f, rs2, make_float2(off[q], off[q]));
+                } else {
+                    f = __fmul2_rn(make_float2(__int2float_rn((int)r0), __int2float_rn((int)r1)), rs2);
+                }
+                float2 &s = sums.v[q][b / 2 * 4 + j];
+                s = __ffma2_rn(f, c, s);
+            }
+        }
+    }
+}
+template <int CW>
+__device__ __forceinline__ void promote(uint32_t taddr, float rs, const float *cs, Sums<CW, true> &sums)
+{
+    constexpr int LD = CW < 16 ? CW : 16;
+    const float2 rs2 = make_float2(rs, rs);
+    uint32_t rr[2][LD];
+    auto fetch = [&](int h) {
+        if constexpr (LD == 16) ptx::tmem_ld_x16(taddr + (uint32_t)(LD * h), rr[h & 1]);
+        else ptx::tmem_ld_x8(taddr + (uint32_t)(LD * h), rr[h & 1]);
+    };
+    fetch(0);
+#pragma unroll
+    for (int h = 0; h < CW / LD; ++h) {
+        uint32_t (&r)[LD] = rr[h & 1];
+        ptx::tmem_ld_wait(r);
+        if (h + 1 < CW / LD) fetch(h + 1);
+#pragma unroll
+        for (int i = 0; i < LD; i += 4) {
+            const float4 c4 = *reinterpret_cast<const float4 *>(cs + LD * h + i);
+            const int k = (LD * h + i) / 2;
+            const float2 f0 = make_float2(__int2float_rn((int)r[i]), __int2float_rn((int)r[i + 1]));
+            const float2 f1 = make_float2(__int2float_rn((int)r[i + 2]), __int2float_rn((int)r[i + 3]));
+            sums.v[k] = __ffma2_rn(__fmul2_rn(f0, rs2), make_float2(c4.x, c4.y), sums.v[k]);
+            sums.v[k + 1] = __ffma2_rn(__fmul2_rn(f1, rs2), make_float2(c4.z, c4.w), sums.v[k + 1]);
+        }
+    }
+}
+
 // The code of an epilogue runs once per tile and streams through the instruction cache: what is unrolled over the columns
 // of a thread is kept to moving registers (a first version, unrolled as a whole, took 15 us for 128 columns).
 //
-// CW columns of z that a thread holds for row `row0 + lane`, from column k0 on: PATCH_COLS at a time through the warp's
-// patch of shared memory, so that lanes write neighbouring pieces of a row.  The pitch of 36 (20) floats keeps 16-byte
-// accesses of eight lanes on different banks.
-template <int CW, int COLS>
+// A warp's 32 rows from row0 on, CW columns of z from column k0 on: 32 at a time through the warp's
+// patch of shared memory, so that lanes write neighbouring pieces of a row.  The pitch of 40 floats keeps the 8-byte writes
+// of sixteen lanes on different banks; reads of eight lanes are 16 bytes of two rows, of which one takes its upper half first.
+template <int CW>
 __device__ __forceinline__ void finish_rows(const OutArgs &o, float *patch, int lane, int row0, int k0,
-                                            const float2 (&acc)[CW / 2])
+                                            const Sums<CW, false> &sums)
 {
-    constexpr int PITCH = COLS + 4, PIECES = COLS / 8;            // pieces of eight columns
+    constexpr int COLS = 32, PITCH = PATCH_PITCH, PIECES = COLS / 8;      // pieces of eight columns
     constexpr int ROWS = 32 / PIECES;                             // rows per step
     const int piece = lane % PIECES, r_in = lane / PIECES;
 #pragma unroll 1
@@ -287,9 +404,11 @@ __device__ __forceinline__ void finish_rows(const OutArgs &o, float *patch, int 
         for (int c = 0; c < CW; c += COLS)
             if (h == c) {
 #pragma unroll
-                for (int i = 0; i < COLS; i += 4)
-                    *reinterpret_cast<float4 *>(patch + lane * PITCH + i) =
-                        make_float4(acc[(c + i) / 2].x, acc[(c + i) / 2].y, acc[(c + i) / 2 + 1].x, acc[(c + i) / 2 + 1].y);
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        *reinterpret_cast<float2 *>(patch + (lane / 4 + 8 * q) * PITCH + 8 * j + 2 * (lane % 4)) =
+                            sums.v[q][c / 8 + j];
             }
         __syncwarp();
         const int k = k0 + h + 8 * piece;                         // first column of this lane's piece
@@ -305,7 +424,9 @@ __device__ __forceinline__ void finish_rows(const OutArgs &o, float *patch, int 
                 if (r >= o.R) continue;
                 float z[8];
                 const float4 *src = reinterpret_cast<const float4 *>(patch + (q + r_in) * PITCH + 8 * piece);
-                const float4 lo = src[0], hi = src[1];
+                const int odd = r_in & 1;
+                const float4 s0 = src[odd], s1 = src[odd ^ 1];
+                const float4 lo = odd ? s1 : s0, hi = odd ? s0 : s1;
                 z[0] = lo.x + b[0]; z[1] = lo.y + b[1]; z[2] = lo.z + b[2]; z[3] = lo.w + b[3];
                 z[4] = hi.x + b[4]; z[5] = hi.y + b[5]; z[6] = hi.z + b[6]; z[7] = hi.w + b[7];
                 if (o.gated) {
@@ -335,7 +456,7 @@ __device__ __forceinline__ void finish_rows(const OutArgs &o, float *patch, int 
 
 // With SWAP a lane has one column k of z for CW rows from r0 on; neighbouring lanes neighbouring columns.
 template <int CW>
-__device__ __forceinline__ void finish_columns(const OutArgs &o, int r0, int k, const float2 (&acc)[CW / 2])
+__device__ __forceinline__ void finish_columns(const OutArgs &o, int r0, int k, const Sums<CW, true> &sums)
 {
     const int half = k & 1, j = o.gated ? k >> 1 : k;
     const bool live = k < o.Kz, mine = live && !(o.gated && half);
@@ -347,7 +468,7 @@ __device__ __forceinline__ void finish_columns(const OutArgs &o, int r0, int k, 
         for (int c = 0; c < CW; c += 8)
             if (h == c) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = (e & 1 ? acc[(c + e) / 2].y : acc[(c + e) / 2].x) + bias;
+                for (int e = 0; e < 8; ++e) y[e] = (e & 1 ? sums.v[(c + e) / 2].y : sums.v[(c + e) / 2].x) + bias;
             }
         const int r = r0 + h;
 #pragma unroll
@@ -373,74 +494,6 @@ __device__ __forceinline__ void finish_columns(const OutArgs &o, int r0, int k, 
     }
 }
 
-// Sums in tensor memory start from the bit pattern of 1.5 * 2^23 instead of zero (MAGIC): read as a float, pattern + sum is
-// 1.5 * 2^23 + sum exactly for |sum| < 2^22, and 127 * 127 * 256 is below that.  The conversion and the product with the row
-// scale are then one multiply-add, f * rs - 1.5 * 2^23 * rs, which is sum * rs rounded once where the second product is
-// exact: the row scale is rounded to 22 bits for that (2^-23 of it at most).  The epilogue writes the pattern back behind
-// its reads.  Against conversions (64 a clock and SM) and two products it halves the issue slots per sum.
-constexpr uint32_t kMagicBits = 0x4b400000u;
-constexpr float kMagic = 12582912.f;
-// With SWAP (few rows of x, bound by the weights' bytes) sums are converted.
-template <bool SWAP> constexpr bool kUseMagic = !SWAP;
-
-__device__ __forceinline__ float round22(float s)
-{
-    const uint32_t u = __float_as_uint(s);
-    return s < 3e38f ? __uint_as_float((u + 1 + ((u >> 2) & 1)) & ~3u) : s;      // to nearest even; scales are not negative
-}
-
-// One piece: CW columns of a lane's row, 16 at a time with the next 16 on their way.  BIG: row scales whose product with
-// 1.5 * 2^23 could overflow.
-template <int CW, bool MAGIC, bool BIG>
-__device__ __forceinline__ void promote(uint32_t taddr, float rs, const float *cs, float2 (&acc)[CW / 2])
-{
-    constexpr int LD = CW < 16 ? CW : 16;
-    const float2 rs2 = make_float2(rs, rs);
-    const float off = -kMagic * rs;
-    const float2 off2 = make_float2(off, off), magic2 = make_float2(-kMagic, -kMagic);
-    uint32_t rr[2][LD];
-    auto fetch = [&](int h) {
-        if constexpr (LD == 16) ptx::tmem_ld_x16(taddr + (uint32_t)(LD * h), rr[h & 1]);
-        else ptx::tmem_ld_x8(taddr + (uint32_t)(LD * h), rr[h & 1]);
-    };
-    uint32_t pattern[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) pattern[i] = kMagicBits;
-    fetch(0);
-#pragma unroll
-    for (int h = 0; h < CW / LD; ++h) {
-        uint32_t (&r)[LD] = rr[h & 1];
-        ptx::tmem_ld_wait(r);
-        if (h + 1 < CW / LD) fetch(h + 1);
-        if constexpr (MAGIC) {
-#pragma unroll
-            for (int i = 0; i < LD; i += 8) ptx::tmem_st_x8(taddr + (uint32_t)(LD * h + i), pattern);
-        }
-#pragma unroll
-        for (int i = 0; i < LD; i += 4) {
-            const float4 c4 = *reinterpret_cast<const float4 *>(cs + LD * h + i);
-            const int k = (LD * h + i) / 2;
-            float2 f0, f1;
-            if constexpr (MAGIC) {
-                f0 = make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
-                f1 = make_float2(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
-                if constexpr (BIG) {
-                    f0 = __fmul2_rn(__fadd2_rn(f0, magic2), rs2);
-                    f1 = __fmul2_rn(__fadd2_rn(f1, magic2), rs2);
-                } else {
-                    f0 = __ffma2_rn(f0, rs2, off2);
-                    f1 = __ffma2_rn(f1, rs2, off2);
-                }
-            } else {
-                f0 = __fmul2_rn(make_float2(__int2float_rn((int)r[i]), __int2float_rn((int)r[i + 1])), rs2);
-                f1 = __fmul2_rn(make_float2(__int2float_rn((int)r[i + 2]), __int2float_rn((int)r[i + 3])), rs2);
-            }
-            acc[k] = __ffma2_rn(f0, make_float2(c4.x, c4.y), acc[k]);
-            acc[k + 1] = __ffma2_rn(f1, make_float2(c4.z, c4.w), acc[k + 1]);
-        }
-    }
-}
-
 // What an epilogue warp keeps through the kernel.
 struct EpiCtx {
     uint32_t tmem;               // its lanes and first column in tensor memory
@@ -448,6 +501,7 @@ struct EpiCtx {
     float *patch, *partial;
     uint32_t free_bar;           // slot_free[0]: this CTA's, or with PAIR the leader's
     int c0, quarter, lane;       // first column of the tile that is this warp's
+    uint32_t pattern[8];         // kMagicBits
 };
 
 template <int BN, bool SWAP, bool PAIR>
@@ -460,9 +514,8 @@ __device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, cons
     const int quarter = ec.quarter, lane = ec.lane;
     // A warp without rows or columns of z still writes the pattern back
     const bool active = row0 + quarter * 32 < a.rows && col0 + ec.c0 < a.cols;
-    float2 acc[CW / 2];
-#pragma unroll
-    for (int j = 0; j < CW / 2; ++j) acc[j] = make_float2(0.f, 0.f);
+    Sums<CW, SWAP> sums;
+    sums.zero();
     for (int q0 = 0; q0 < rg.np; q0 += a.cg) {
         const int n = min(a.cg, rg.np - q0);
         if (!wait<C>(ptx::smem_u32(&sh->acc_full[slot]), sphase, ctx, kWaitTmemFull)) return false;
@@ -471,14 +524,22 @@ __device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, cons
             const float *sc = ec.scales + (size_t)slot * C::SLOT_SCALE_FLOATS;
             for (int j = 0; j < n; ++j) {
                 const uint32_t taddr = ec.tmem + (uint32_t)(slot * SLOT_COLS + j * BN);
+                const float *rows = sc + j * C::GROUP_SCALE_FLOATS + quarter * 32;
                 const float *cs = sc + j * C::GROUP_SCALE_FLOATS + BM + ec.c0;
-                float rs = sc[j * C::GROUP_SCALE_FLOATS + quarter * 32 + lane];
-                if constexpr (MAGIC) {
-                    rs = round22(rs);
-                    if (__any_sync(0xffffffffu, !(rs < 1e30f))) promote<CW, true, true>(taddr, rs, cs, acc);
-                    else promote<CW, true, false>(taddr, rs, cs, acc);
+                if constexpr (SWAP) {
+                    promote<CW>(taddr, rows[lane], cs, sums);
                 } else {
-                    promote<CW, false, false>(taddr, rs, cs, acc);
+                    float rs[4];
+                    bool big = false;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {       // scales behind the last row are not written
+                        rs[q] = row0 + quarter * 32 + lane / 4 + 8 * q < a.rows ? rows[lane / 4 + 8 * q] : 0.f;
+                        if (MAGIC) rs[q] = round22(rs[q]);
+                        big |= !(rs[q] < 1e30f);
+                    }
+                    cs += 2 * (lane % 4);
+                    if (MAGIC && __any_sync(0xffffffffu, big)) promote<CW, MAGIC, true>(taddr, rs, cs, ec.pattern, sums);
+                    else promote<CW, MAGIC, false>(taddr, rs, cs, ec.pattern, sums);
                 }
             }
             if constexpr (MAGIC) ptx::tmem_st_wait();
@@ -498,15 +559,26 @@ __device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, cons
     }
     if constexpr (!PAIR) {
         if (a.split > 1) {           // [column][lane of TMEM], one float of padding per column
+            float *to = ec.partial + ec.c0 * (BM + 1) + quarter * 32;
+            if constexpr (SWAP) {
 #pragma unroll
-            for (int j = 0; j < CW; ++j)
-                ec.partial[(ec.c0 + j) * (BM + 1) + quarter * 32 + lane] = j & 1 ? acc[j / 2].y : acc[j / 2].x;
+                for (int j = 0; j < CW; ++j) to[j * (BM + 1) + lane] = j & 1 ? sums.v[j / 2].y : sums.v[j / 2].x;
+            } else {
+                to += 2 * (lane % 4) * (BM + 1) + lane / 4;
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int j = 0; j < CW / 8; ++j) {
+                        to[8 * j * (BM + 1) + 8 * q] = sums.v[q][j].x;
+                        to[(8 * j + 1) * (BM + 1) + 8 * q] = sums.v[q][j].y;
+                    }
+            }
             return true;
         }
     }
     if (active) {
-        if constexpr (SWAP) finish_columns<CW>(a.out, col0 + ec.c0, row0 + quarter * 32 + lane, acc);
-        else finish_rows<CW, C::PATCH_COLS>(a.out, ec.patch, lane, row0 + quarter * 32, col0 + ec.c0, acc);
+        if constexpr (SWAP) finish_columns<CW>(a.out, col0 + ec.c0, row0 + quarter * 32 + lane, sums);
+        else finish_rows<CW>(a.out, ec.patch, lane, row0 + quarter * 32, col0 + ec.c0, sums);
     }
     return true;
 }
@@ -775,13 +847,14 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         if constexpr (PAIR) ec.free_bar = ptx::map_rank(ec.free_bar, 0);
         ec.quarter = quarter;
         ec.lane = lane;
+        // kept in registers: as constants they are moved into place again for every store
+#pragma unroll
+        for (int i = 0; i < 8; ++i) asm volatile("mov.b32 %0, %1;" : "=r"(ec.pattern[i]) : "n"(kMagicBits));
         if constexpr (MAGIC) {
             // the slots start from the pattern: this warp's lanes and columns of every piece
-            uint32_t pattern[8];
-            for (int i = 0; i < 8; ++i) pattern[i] = kMagicBits;
             for (int s = 0; s < NSLOT; ++s)
                 for (int c = 0; c < C::CG_MAX * BN; c += BN)
-                    for (int i = 0; i < BN / 2; i += 8) ptx::tmem_st_x8(ec.tmem + (uint32_t)(s * SLOT_COLS + c + i), pattern);
+                    for (int i = 0; i < BN / 2; i += 8) ptx::tmem_st_x8(ec.tmem + (uint32_t)(s * SLOT_COLS + c + i), ec.pattern);
             ptx::tmem_st_wait();
             ptx::tc_fence_before();
             __syncwarp();

@@ -380,6 +380,19 @@ __device__ __forceinline__ void tmem_ld_x8(uint32_t taddr, uint32_t (&r)[8])
         : "r"(taddr)
         : "memory");
 }
+// 16 lanes x 32 columns as 16x256b: thread i gets, for every 8 columns j, columns 8 j + 2 (i % 4) and the next one of lane
+// i / 4 in r[4 j], r[4 j + 1] and of lane i / 4 + 8 in r[4 j + 2], r[4 j + 3].
+__device__ __forceinline__ void tmem_ld_16x256b_x4(uint32_t taddr, uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+          "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
 // Store: thread i of the warp writes 8 consecutive 32-bit columns of lane (base + i).
 __device__ __forceinline__ void tmem_st_x8(uint32_t taddr, const uint32_t (&r)[8])
 {
@@ -457,7 +470,7 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
 // Arrive on a barrier of any CTA of the cluster (a cluster address).
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // Registers of a warpgroup: less for the roles that move data, more for those that hold sums.
 template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
