@@ -267,22 +267,6 @@ __device__ __forceinline__ void activate_all(float (&z)[N], int act)
     }
 }
 
-// Sums in tensor memory start from the bit pattern of 1.5 * 2^23 instead of zero (MAGIC): read as a float, pattern + sum is
-// 1.5 * 2^23 + sum exactly for |sum| < 2^22, and 127 * 127 * 256 is below that.  The conversion and the product with the row
-// scale are then one multiply-add, f * rs - 1.5 * 2^23 * rs, which is sum * rs rounded once where the second product is
-// exact: the row scale is rounded to 22 bits for that (2^-23 of it at most).  The epilogue writes the pattern back behind
-// its reads.  Against conversions (64 a clock and SM) and two products it halves the issue slots per sum.
-constexpr uint32_t kMagicBits = 0x4b400000u;
-constexpr float kMagic = 12582912.f;
-// With SWAP (few rows of x, bound by the weights' bytes) sums are converted.
-template <bool SWAP> constexpr bool kUseMagic = !SWAP;
-
-__device__ __forceinline__ float round22(float s)
-{
-    const uint32_t u = __float_as_uint(s);
-    return s < 3e38f ? __uint_as_float((u + 1 + ((u >> 2) & 1)) & ~3u) : s;      // to nearest even; scales are not negative
-}
-
 // The sums of an epilogue warp, 32 rows of TMEM lanes x CW columns.  Where there are many columns (!SWAP) a thread has four
 // rows, lane / 4 + 8 q, and every fourth pair of columns, 8 j + 2 (lane % 4): a column scale is then read from shared
 // memory by four threads instead of by all 32.  With a row per thread the reads return CW floats to every lane, 1024 cycles
@@ -308,50 +292,37 @@ template <int CW> struct Sums<CW, true> {
     }
 };
 
-// One piece, 32 columns at a time, 16 lanes after the other, with the next load on its way.  `rs`: scales of the thread's
-// rows; `cs`: the warp's column scales, from the thread's first column on.  BIG: row scales whose product with 1.5 * 2^23
-// could overflow.
-template <int CW, bool MAGIC, bool BIG>
-__device__ __forceinline__ void promote(uint32_t taddr, const float (&rs)[4], const float *cs, const uint32_t (&pattern)[8],
-                                        Sums<CW, false> &sums)
+// One piece: int32 sums to fp32, times the row scale, times the column scale, added.  Up to 64 columns at a time, 16 lanes
+// after the other, with the next load on its way.  `rs`: scales of the thread's rows; `cs`: the warp's column scales, from
+// the thread's first column on.
+template <int CW>
+__device__ __forceinline__ void promote(uint32_t taddr, const float (&rs)[4], const float *cs, Sums<CW, false> &sums)
 {
-    float off[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) off[q] = -kMagic * rs[q];
-    uint32_t rr[2][16];
-    auto fetch = [&](int b) {      // block b: columns 32 (b / 2) on, lanes 16 (b % 2) on
-        ptx::tmem_ld_16x256b_x4(taddr + (uint32_t)(b / 2 * 32) + ((uint32_t)(b % 2 * 16) << 16), rr[b & 1]);
+    constexpr int LC = CW < 64 ? CW : 64;        // columns of a load
+    uint32_t rr[2][LC / 2];
+    float2 c[LC / 8];
+    auto fetch = [&](int b) {                    // block b: columns LC (b / 2) on, lanes 16 (b % 2) on
+        ptx::tmem_ld_16x256b(taddr + (uint32_t)(b / 2 * LC) + ((uint32_t)(b % 2 * 16) << 16), rr[b & 1]);
     };
     fetch(0);
 #pragma unroll
-    for (int b = 0; b < CW / 16; ++b) {
-        uint32_t (&r)[16] = rr[b & 1];
-        ptx::tmem_ld_wait(r);
-        if (b + 1 < CW / 16) fetch(b + 1);
-        if constexpr (MAGIC) {
-            if (b % 2) {           // all 32 lanes of these columns have been read
+    for (int b = 0; b < 2 * CW / LC; ++b) {
+        uint32_t (&r)[LC / 2] = rr[b & 1];
+        if (b % 2 == 0) {
 #pragma unroll
-                for (int i = 0; i < 32; i += 8) ptx::tmem_st_x8(taddr + (uint32_t)(b / 2 * 32 + i), pattern);
-            }
+            for (int j = 0; j < LC / 8; ++j) c[j] = *reinterpret_cast<const float2 *>(cs + b / 2 * LC + 8 * j);
         }
+        ptx::tmem_ld_wait(r);
+        if (b + 1 < 2 * CW / LC) fetch(b + 1);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float2 c = *reinterpret_cast<const float2 *>(cs + b / 2 * 32 + 8 * j);
+        for (int h = 0; h < 2; ++h) {
+            const int q = b % 2 * 2 + h;
+            const float2 rs2 = make_float2(rs[q], rs[q]);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int q = b % 2 * 2 + h;
-                const uint32_t r0 = r[4 * j + 2 * h], r1 = r[4 * j + 2 * h + 1];
-                const float2 rs2 = make_float2(rs[q], rs[q]);
-                float2 f;
-                if constexpr (MAGIC) {
-                    f = make_float2(__uint_as_float(r0), __uint_as_float(r1));
-                    if constexpr (BIG) f = __fmul2_rn(__fadd2_rn(f, make_float2(-kMagic, -kMagic)), rs2);
-                    else f = __ffma2_rn(f, rs2, make_float2(off[q], off[q]));
-                } else {
-                    f = __fmul2_rn(make_float2(__int2float_rn((int)r0), __int2float_rn((int)r1)), rs2);
-                }
-                float2 &s = sums.v[q][b / 2 * 4 + j];
-                s = __ffma2_rn(f, c, s);
+            for (int j = 0; j < LC / 8; ++j) {
+                const float2 f = make_float2(__int2float_rn((int)r[4 * j + 2 * h]), __int2float_rn((int)r[4 * j + 2 * h + 1]));
+                float2 &s = sums.v[q][b / 2 * (LC / 8) + j];
+                s = __ffma2_rn(__fmul2_rn(f, rs2), c[j], s);
             }
         }
     }
@@ -501,7 +472,6 @@ struct EpiCtx {
     float *patch, *partial;
     uint32_t free_bar;           // slot_free[0]: this CTA's, or with PAIR the leader's
     int c0, quarter, lane;       // first column of the tile that is this warp's
-    uint32_t pattern[8];         // kMagicBits
 };
 
 template <int BN, bool SWAP, bool PAIR>
@@ -509,18 +479,17 @@ __device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, cons
                                               int col0, const Range &rg, int &slot, uint32_t &sphase)
 {
     using C = Cfg<BN, SWAP, PAIR>;
-    constexpr bool MAGIC = kUseMagic<SWAP>;
     constexpr int CW = BN / 2;                    // columns of a warp
     const int quarter = ec.quarter, lane = ec.lane;
-    // A warp without rows or columns of z still writes the pattern back
+    // warp-uniform: does this warp have rows and columns of z?
     const bool active = row0 + quarter * 32 < a.rows && col0 + ec.c0 < a.cols;
     Sums<CW, SWAP> sums;
     sums.zero();
     for (int q0 = 0; q0 < rg.np; q0 += a.cg) {
         const int n = min(a.cg, rg.np - q0);
         if (!wait<C>(ptx::smem_u32(&sh->acc_full[slot]), sphase, ctx, kWaitTmemFull)) return false;
-        ptx::tc_fence_after();
-        if (active || MAGIC) {
+        if (active) {
+            ptx::tc_fence_after();
             const float *sc = ec.scales + (size_t)slot * C::SLOT_SCALE_FLOATS;
             for (int j = 0; j < n; ++j) {
                 const uint32_t taddr = ec.tmem + (uint32_t)(slot * SLOT_COLS + j * BN);
@@ -530,19 +499,11 @@ __device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, cons
                     promote<CW>(taddr, rows[lane], cs, sums);
                 } else {
                     float rs[4];
-                    bool big = false;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {       // scales behind the last row are not written
-                        rs[q] = row0 + quarter * 32 + lane / 4 + 8 * q < a.rows ? rows[lane / 4 + 8 * q] : 0.f;
-                        if (MAGIC) rs[q] = round22(rs[q]);
-                        big |= !(rs[q] < 1e30f);
-                    }
-                    cs += 2 * (lane % 4);
-                    if (MAGIC && __any_sync(0xffffffffu, big)) promote<CW, MAGIC, true>(taddr, rs, cs, ec.pattern, sums);
-                    else promote<CW, MAGIC, false>(taddr, rs, cs, ec.pattern, sums);
+                    for (int q = 0; q < 4; ++q) rs[q] = rows[lane / 4 + 8 * q];
+                    promote<CW>(taddr, rs, cs + 2 * (lane % 4), sums);
                 }
             }
-            if constexpr (MAGIC) ptx::tmem_st_wait();
             ptx::tc_fence_before();
         }
         __syncwarp();
@@ -593,15 +554,13 @@ __device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tm
     using C = Cfg<BN, SWAP, PAIR>;
     constexpr uint32_t dhi = ptx::smem_desc_sw128_hi();
     constexpr uint32_t idesc = ptx::idesc_i8(PAIR ? 2 * BM : BM, BN);
-    constexpr bool MAGIC = kUseMagic<SWAP>;                              // sums are added to what the epilogue wrote
-    constexpr uint32_t FIRST = MAGIC ? 0u : 1u;                          // the epilogue has to have freed a slot first
     constexpr int PER = GST == 1 || GST == 2 ? 4 / GST : 1;              // groups per stage
     constexpr int CG = PER < C::CG_MAX ? PER : C::CG_MAX;                // pieces per chunk
     const uint32_t full0 = ptx::smem_u32(&sh->full[0]), empty0 = ptx::smem_u32(&sh->empty[0]);
     const uint32_t acc0 = ptx::smem_u32(&sh->acc_full[0]), free0 = ptx::smem_u32(&sh->slot_free[0]);
     auto mma = [&](uint32_t d, uint32_t al, uint32_t bl, bool first_step) {
-        if constexpr (PAIR) ptx::umma_i8_pair(d, al, bl, dhi, idesc, MAGIC || !first_step);
-        else ptx::umma_i8_lo(d, al, bl, dhi, idesc, MAGIC || !first_step);
+        if constexpr (PAIR) ptx::umma_i8_pair(d, al, bl, dhi, idesc, !first_step);
+        else ptx::umma_i8_lo(d, al, bl, dhi, idesc, !first_step);
     };
     auto commit = [&](uint32_t bar) {
         if constexpr (PAIR) ptx::umma_commit_pair(bar);
@@ -618,7 +577,7 @@ __device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tm
             const uint32_t a_lo = tiles_lo + (uint32_t)(stage * (C::STAGE_BYTES >> 4));
             const uint32_t b_lo = a_lo + (uint32_t)(A_BYTES >> 4);
             if constexpr (GST == 4) {
-                if (begins && !wait<C>(free0 + 8u * slot, sphase ^ FIRST, ctx, kWaitTmemEmpty)) return;
+                if (begins && !wait<C>(free0 + 8u * slot, sphase ^ 1u, ctx, kWaitTmemEmpty)) return;
                 in_group += n;
                 const bool ends = in_group == a.gsteps || in_group % PIECE == 0 || 4 * kb + n == rg.s1;
                 ptx::tc_fence_after();
@@ -641,7 +600,7 @@ __device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tm
 #pragma unroll
                 for (int c = 0; c < 4; c += CG * GST) {                  // chunks of the stage
                     if (c < n) {
-                        if (!wait<C>(free0 + 8u * slot, sphase ^ FIRST, ctx, kWaitTmemEmpty)) return;
+                        if (!wait<C>(free0 + 8u * slot, sphase ^ 1u, ctx, kWaitTmemEmpty)) return;
                         ptx::tc_fence_after();
                         if (ptx::elect_one()) {
                             const uint32_t d = tmem_base + (uint32_t)(slot * SLOT_COLS);
@@ -663,7 +622,7 @@ __device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tm
                 ptx::tc_fence_after();
                 for (int s = 0; s < n; ++s) {
                     if (begins) {
-                        if (!wait<C>(free0 + 8u * slot, sphase ^ FIRST, ctx, kWaitTmemEmpty)) return;
+                        if (!wait<C>(free0 + 8u * slot, sphase ^ 1u, ctx, kWaitTmemEmpty)) return;
                         ptx::tc_fence_after();
                     }
                     const bool ends = ++in_group == a.gsteps || in_group % PIECE == 0 || 4 * kb + s + 1 == rg.s1;
@@ -692,7 +651,6 @@ __global__ void __launch_bounds__(THREADS, 1)
 linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, MmaArgs a)
 {
     using C = Cfg<BN, SWAP, PAIR>;
-    constexpr bool MAGIC = kUseMagic<SWAP>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *tiles = ptx::align_smem<1024>(smem_raw);
     float *patches = reinterpret_cast<float *>(tiles + (size_t)C::STAGES * C::STAGE_BYTES);
@@ -803,7 +761,7 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             const long long row0 = min((long long)mt * row_block + row_off, a.row_pitch - BM);
             for (int q0 = 0; q0 < rg.np; q0 += a.cg) {
                 const int n = min(a.cg, rg.np - q0);
-                ok = wait<C>(scale_bar + 8u * slot, sphase ^ (MAGIC ? 0u : 1u), ctx, kWaitScaleEmpty);
+                ok = wait<C>(scale_bar + 8u * slot, sphase ^ 1u, ctx, kWaitScaleEmpty);
                 if (!ok) break;
                 const uint32_t bar = ptx::smem_u32(&sh->acc_full[slot]);
                 const uint32_t dst = ptx::smem_u32(scales + (size_t)slot * C::SLOT_SCALE_FLOATS);
@@ -847,29 +805,6 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         if constexpr (PAIR) ec.free_bar = ptx::map_rank(ec.free_bar, 0);
         ec.quarter = quarter;
         ec.lane = lane;
-        // kept in registers: as constants they are moved into place again for every store
-#pragma unroll
-        for (int i = 0; i < 8; ++i) asm volatile("mov.b32 %0, %1;" : "=r"(ec.pattern[i]) : "n"(kMagicBits));
-        if constexpr (MAGIC) {
-            // the slots start from the pattern: this warp's lanes and columns of every piece
-            for (int s = 0; s < NSLOT; ++s)
-                for (int c = 0; c < C::CG_MAX * BN; c += BN)
-                    for (int i = 0; i < BN / 2; i += 8) ptx::tmem_st_x8(ec.tmem + (uint32_t)(s * SLOT_COLS + c + i), ec.pattern);
-            ptx::tmem_st_wait();
-            ptx::tc_fence_before();
-            __syncwarp();
-            if (ptx::elect_one()) {
-                for (int s = 0; s < NSLOT; ++s) {
-                    if constexpr (PAIR) {
-                        ptx::mbar_arrive(ptx::smem_u32(&sh->scale_free[s]));
-                        ptx::mbar_arrive_cluster(ec.free_bar + 8u * s);
-                    } else {
-                        ptx::mbar_arrive(ec.free_bar + 8u * s);
-                    }
-                }
-            }
-            __syncwarp();
-        }
         for (int t = first; t < a.tiles; t += stride) {
             const int mt = t % a.MT, nt = t / a.MT;
             if (!epilogue_tile<BN, SWAP, PAIR>(sh, a, ctx, ec, mt * row_block + row_off, nt * BN, rg, slot, sphase)) break;
