@@ -84,7 +84,7 @@ struct Cfg {
     static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
     static_assert(PAIR || (size_t)BN * (BM + 1) * 4 <= (size_t)STAGES * STAGE_BYTES, "partial sums fit the stages");
     // Registers behind setmaxnreg: the epilogue holds BN / 2 sums and two blocks of loads.
-    // 128 * 40 + 256 * 232 = 384 * 168, what the block is launched with.
+    // 128 * 56 + 256 * 216 <= 384 * 168, what the block is launched with.
     static constexpr bool MOVE_REGS = PAIR && BN == 256;
 };
 
@@ -701,7 +701,7 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     ptx::grid_launch_dependents();
 
     if (warp < FIRST_EPI_WARP) {
-    if constexpr (C::MOVE_REGS) ptx::fewer_registers<40>();
+    if constexpr (C::MOVE_REGS) ptx::fewer_registers<56>();
     if (warp == 0) {
         // ---------------- TMA producer ----------------
         int stage = 0;
@@ -791,7 +791,7 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     }
     } else {
         // ---------------- epilogue ----------------
-        if constexpr (C::MOVE_REGS) ptx::more_registers<232>();
+        if constexpr (C::MOVE_REGS) ptx::more_registers<216>();
         const int e = warp - FIRST_EPI_WARP, quarter = warp & 3;
         int slot = 0;
         uint32_t sphase = 0;
