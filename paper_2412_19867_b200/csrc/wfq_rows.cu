@@ -36,18 +36,6 @@ template <> struct Elem<__nv_bfloat16> {
 };
 
 // Eight consecutive elements, 16-byte aligned.
-template <typename T> __device__ __forceinline__ void load8(const T *p, float (&v)[8])
-{
-    if constexpr (sizeof(T) == 4) {
-        const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
-        const uint4 a = *reinterpret_cast<const uint4 *>(p);
-        const T *e = reinterpret_cast<const T *>(&a);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = Elem<T>::get(e[i]);
-    }
-}
 template <typename T> __device__ __forceinline__ void store8(T *p, const float (&v)[8])
 {
     if constexpr (sizeof(T) == 4) {
@@ -156,12 +144,22 @@ __global__ void __launch_bounds__(256) rows_any_kernel(RowsArgs a)
     }
 }
 
-// VEC consecutive elements as fp32 (VEC 8: 16-byte aligned).
-template <int VEC, typename T> __device__ __forceinline__ void load(const T *p, float (&v)[VEC])
-{
-    if constexpr (VEC == 8) load8(p, v);
-    else v[0] = Elem<T>::get(*p);
-}
+// VEC consecutive elements as they lie in memory (VEC 8: 16-byte aligned).
+template <typename T, int VEC> struct Raw {
+    uint4 q[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T *p)
+    {
+        const uint4 *src = reinterpret_cast<const uint4 *>(p);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) q[i] = src[i];
+    }
+    __device__ __forceinline__ float get(int e) const { return Elem<T>::get(reinterpret_cast<const T *>(q)[e]); }
+};
+template <typename T> struct Raw<T, 1> {
+    T v;
+    __device__ __forceinline__ void load(const T *p) { v = *p; }
+    __device__ __forceinline__ float get(int) const { return Elem<T>::get(v); }
+};
 template <int VEC, typename T> __device__ __forceinline__ void store(T *p, const float (&v)[VEC])
 {
     if constexpr (VEC == 8) store8(p, v);
@@ -171,127 +169,173 @@ template <int VEC, typename T> __device__ __forceinline__ void store(T *p, const
 // Rows of up to 32768 channels, held in registers: one pass.  `tpr` threads (whole warps) have a row, thread t the
 // vectors t, t + tpr, ... of VEC elements; a CTA has several short rows.  A group of gs = VEC * lanes channels (lanes a
 // power of two up to 32) lies in neighbouring lanes; other groups are joined in shared memory (`direct` 0).
-template <typename T, bool NORM, bool RES, int VEC, int NV>
-__global__ void __launch_bounds__(1024) rows_kernel(RowsArgs a, int tpr, int lanes, int direct)
+// Bound by memory: CTAs walk over the rows and ask for the next one's values before they work on this one's, so that
+// loads are on their way throughout; the gain stays in registers.
+template <typename T, bool NORM, bool RES, int VEC, int NV, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? 3 : 1) rows_kernel(RowsArgs a, int tpr, int lanes, int direct)
 {
-    extern __shared__ int group_max[];        // [rows of the CTA][G] where groups are joined
-    __shared__ float warp_sum[32];
+    extern __shared__ int group_max[];        // [2][rows of the CTA][G] where groups are joined, alternately
+    __shared__ float warp_sum[2][32];
     const int local = (int)threadIdx.x / tpr, t = (int)threadIdx.x - local * tpr, per_cta = (int)blockDim.x / tpr;
-    const long long row = (long long)blockIdx.x * per_cta + local;
-    const bool live = row < a.rows;
     const int lane = threadIdx.x & 31;
-    int *gmax = group_max + local * a.G;
+    const int n = a.C / VEC;                  // vectors of a row
+    const long long step = (long long)gridDim.x * per_cta;
+    const long long rounds = (a.rows + step - 1) / step;      // the same for all threads: they meet at barriers
     if (!direct) {
-        for (int g = t; g < a.G; g += tpr) gmax[g] = 0;
+        for (int i = threadIdx.x; i < 2 * per_cta * a.G; i += blockDim.x) group_max[i] = 0;
         __syncthreads();
     }
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
 
-    float u[NV][VEC];
-    float sum = 0.f;
-    const int n = live ? a.C / VEC : 0;       // vectors of the row
-    const T *x = static_cast<const T *>(a.x) + row * a.ldx;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int v = i * tpr + t;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) u[i][e] = 0.f;
-        if (v < n) load<VEC>(x + v * VEC, u[i]);
-    }
-    if constexpr (RES) {
-        const T *r = static_cast<const T *>(a.residual) + row * a.ldr;
-        T *h = static_cast<T *>(a.h) + row * a.ldh;
-        float w[NV][VEC];
+    Raw<T, VEC> x[NV], r[RES ? NV : 1];
+    float gain[NORM ? NV : 1][VEC];
+    auto ask = [&](long long row) {
+        if (row >= a.rows) return;
+        const T *px = static_cast<const T *>(a.x) + row * a.ldx;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (i * tpr + t < n) load<VEC>(r + (i * tpr + t) * VEC, w[i]);
+            if (i * tpr + t < n) x[i].load(px + (i * tpr + t) * VEC);
+        if constexpr (RES) {
+            const T *pr = static_cast<const T *>(a.residual) + row * a.ldr;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (i * tpr + t < n) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) u[i][e] = Elem<T>::get(Elem<T>::put(__fadd_rn(u[i][e], w[i][e])));
-                if (a.h) store<VEC>(h + (i * tpr + t) * VEC, u[i]);
-            }
-    }
-    int amax[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int v = i * tpr + t;
-        if constexpr (NORM) {
-            float gain[VEC];
-            if (v < n) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) sum = fmaf(u[i][e], u[i][e], sum);
-                load<VEC>(a.gain + v * VEC, gain);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) u[i][e] = __fmul_rn(u[i][e], gain[e]);
-            }
+            for (int i = 0; i < NV; ++i)
+                if (i * tpr + t < n) r[i].load(pr + (i * tpr + t) * VEC);
         }
-        amax[i] = 0;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) amax[i] = max(amax[i], magnitude_bits(u[i][e]));
-        for (int o = 1; o < lanes; o <<= 1) amax[i] = max(amax[i], __shfl_xor_sync(0xffffffffu, amax[i], o));
-        if (!direct && v < n && (lane & (lanes - 1)) == 0) atomicMax(&gmax[v * VEC / a.gs], amax[i]);
-    }
-    float rstd = 1.f;
+    };
+    long long row = (long long)blockIdx.x * per_cta + local;
+    ask(row);
     if constexpr (NORM) {
 #pragma unroll
-        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (tpr > 32) {
-            if (lane == 0) warp_sum[threadIdx.x >> 5] = sum;
-            __syncthreads();
-            sum = 0.f;
-            for (int w = 0; w < tpr / 32; ++w) sum += warp_sum[local * (tpr / 32) + w];
+        for (int i = 0; i < NV; ++i) {
+            const int v = i * tpr + t;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) gain[i][e] = v < n ? __ldg(a.gain + v * VEC + e) : 0.f;
         }
-        rstd = rstd_of(sum, a);
     }
-    if (!direct && !(NORM && tpr > 32)) __syncthreads();
-    if (!live) return;
-    const int to = target_row(a, (int)row);
-    int8_t *codes = a.codes + (size_t)to * a.Cp;
+    for (long long k = 0; k < rounds; ++k, row += step) {
+        const bool live = row < a.rows;
+        const int odd = (int)(k & 1);
+        int *gmax = group_max + (odd * per_cta + local) * a.G;
+        float u[NV][VEC];
+        float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int v = i * tpr + t;
-        if (v >= a.Cp / VEC) break;
-        const int g = v * VEC / a.gs;
-        float scale, inv;
-        scale_of(direct ? amax[i] : gmax[g], scale, inv);
-        if (v * VEC == g * a.gs) a.scales[(size_t)g * a.scale_pitch + to] = NORM ? __fmul_rn(scale, rstd) : scale;
-        uint32_t w[VEC];
+        for (int i = 0; i < NV; ++i) {
+            const bool has = live && i * tpr + t < n;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) w[e] = inv > 0.f ? code_bits(u[i][e], inv) : 0u;
-        if constexpr (VEC == 8) {
-            const uint32_t lo = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
-            const uint32_t hi = __byte_perm(__byte_perm(w[4], w[5], 0x0040), __byte_perm(w[6], w[7], 0x0040), 0x5410);
-            *reinterpret_cast<uint2 *>(codes + v * 8) = make_uint2(lo, hi);
-        } else {
-            codes[v] = (int8_t)w[0];
+            for (int e = 0; e < VEC; ++e) {
+                float h = has ? x[i].get(e) : 0.f;
+                if constexpr (RES) {
+                    if (has) h = Elem<T>::get(Elem<T>::put(__fadd_rn(h, r[i].get(e))));
+                }
+                u[i][e] = h;
+            }
         }
+        ask(row + step);
+        if constexpr (RES) {
+            if (a.h && live) {
+                T *h = static_cast<T *>(a.h) + row * a.ldh;
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if (i * tpr + t < n) store<VEC>(h + (i * tpr + t) * VEC, u[i]);
+            }
+        }
+        int amax[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if constexpr (NORM) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum = fmaf(u[i][e], u[i][e], sum);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) u[i][e] = __fmul_rn(u[i][e], gain[i][e]);
+            }
+            amax[i] = 0;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) amax[i] = max(amax[i], magnitude_bits(u[i][e]));
+            for (int o = 1; o < lanes; o <<= 1) amax[i] = max(amax[i], __shfl_xor_sync(0xffffffffu, amax[i], o));
+            const int v = i * tpr + t;
+            if (!direct && v < n && (lane & (lanes - 1)) == 0) atomicMax(&gmax[v * VEC / a.gs], amax[i]);
+        }
+        if constexpr (NORM) {
+#pragma unroll
+            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (tpr > 32 && lane == 0) warp_sum[odd][threadIdx.x >> 5] = sum;
+        }
+        if (!direct || (NORM && tpr > 32)) __syncthreads();
+        float rstd = 1.f;
+        if constexpr (NORM) {
+            if (tpr > 32) {
+                sum = 0.f;
+                for (int w = 0; w < tpr / 32; ++w) sum += warp_sum[odd][local * (tpr / 32) + w];
+            }
+            rstd = rstd_of(sum, a);
+        }
+        if (!direct) {        // the other half is free: everybody is past last round's reads of it
+            int *other = group_max + ((odd ^ 1) * per_cta + local) * a.G;
+            for (int g = t; g < a.G; g += tpr) other[g] = 0;
+        }
+        if (live) {
+            const int to = target_row(a, (int)row);
+            int8_t *codes = a.codes + (size_t)to * a.Cp;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int v = i * tpr + t;
+                if (v < a.Cp / VEC) {
+                    const int g = v * VEC / a.gs;
+                    float scale, inv;
+                    scale_of(direct ? amax[i] : gmax[g], scale, inv);
+                    if (v * VEC == g * a.gs) a.scales[(size_t)g * a.scale_pitch + to] = NORM ? __fmul_rn(scale, rstd) : scale;
+                    uint32_t w[VEC];
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) w[e] = inv > 0.f ? code_bits(u[i][e], inv) : 0u;
+                    if constexpr (VEC == 8) {
+                        const uint32_t lo = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
+                        const uint32_t hi = __byte_perm(__byte_perm(w[4], w[5], 0x0040), __byte_perm(w[6], w[7], 0x0040), 0x5410);
+                        *reinterpret_cast<uint2 *>(codes + v * 8) = make_uint2(lo, hi);
+                    } else {
+                        codes[v] = (int8_t)w[0];
+                    }
+                }
+            }
+        }
+        if (!direct) __syncthreads();     // the zeros are in place before the next round's maxima
     }
 }
 
-// Codes back to values, VEC of them per thread and step.
+// Codes back to values, VEC of them at a time, four such pieces of a row on their way per thread.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(256) dequantize_kernel(const int8_t *codes, const float *scales, int rows, int C, int Cp,
-                                                         int gs, long long scale_pitch, T *v, long long ldv, int tpr)
+__global__ void __launch_bounds__(256) dequantize_kernel(const int8_t *__restrict__ codes, const float *__restrict__ scales,
+                                                         int rows, int C, int Cp, int gs, long long scale_pitch,
+                                                         T *__restrict__ v, long long ldv, int tpr)
 {
+    constexpr int N = 4;
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-    const int local = (int)threadIdx.x / tpr, per_cta = 256 / tpr;
+    const int local = (int)threadIdx.x / tpr, per_cta = 256 / tpr, t = (int)threadIdx.x - local * tpr;
     if (local >= per_cta) return;
     for (long long row = (long long)blockIdx.x * per_cta + local; row < rows; row += (long long)gridDim.x * per_cta)
-        for (int c = ((int)threadIdx.x - local * tpr) * VEC; c < C; c += tpr * VEC) {
-            const float s = scales[(size_t)(c / gs) * scale_pitch + row];
-            float out[VEC];
-            if constexpr (VEC == 8) {
-                const uint2 q = *reinterpret_cast<const uint2 *>(codes + row * Cp + c);
+        for (int c0 = t * VEC; c0 < C; c0 += N * tpr * VEC) {
+            uint2 q[N];
+            float s[N];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) out[e] = (float)(int8_t)((e < 4 ? q.x : q.y) >> (8 * (e & 3))) * s;
-            } else {
-                out[0] = (float)codes[row * Cp + c] * s;
+            for (int i = 0; i < N; ++i) {
+                const int c = c0 + i * tpr * VEC;
+                if (c < C) {
+                    if constexpr (VEC == 8) q[i] = __ldg(reinterpret_cast<const uint2 *>(codes + row * Cp + c));
+                    else q[i].x = (uint32_t)(uint8_t)__ldg(codes + row * Cp + c);
+                    s[i] = __ldg(scales + (size_t)(c / gs) * scale_pitch + row);
+                }
             }
-            store<VEC>(v + row * ldv + c, out);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int c = c0 + i * tpr * VEC;
+                if (c < C) {
+                    float out[VEC];
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) out[e] = (float)(int8_t)((e < 4 ? q[i].x : q[i].y) >> (8 * (e & 3))) * s[i];
+                    store<VEC>(v + row * ldv + c, out);
+                }
+            }
         }
 }
 
@@ -311,26 +355,57 @@ cudaError_t launch(K kernel, dim3 grid, int threads, size_t smem, cudaStream_t s
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// Threads and vectors per thread of a row, for E elements per thread.
-template <typename T, bool NORM, bool RES, int VEC, int NV>
+// CTAs that fit an SM, from the registers a thread.
+int resident_ctas(int regs, int threads, size_t smem)
+{
+    const int per_warp = (regs * 32 + 255) / 256 * 256;
+    int n = 65536 / (per_warp * (threads / 32));
+    const int by_smem = (int)(200 * 1024 / (smem + 1280));
+    if (by_smem < n) n = by_smem;
+    if (2048 / threads < n) n = 2048 / threads;
+    return n < 1 ? 1 : n;
+}
+
+template <typename T, bool NORM, bool RES, int VEC, int NV, int THREADS>
 cudaError_t launch_rows_kernel(const RowsArgs &a, int tpr, cudaStream_t stream, bool pdl)
 {
     // lanes of the largest power of two of channels that no group's border cuts
-    int lanes = 1;
+    int lanes = 1, sms = 0;
     while (lanes < 32 && a.gs % (2 * lanes * VEC) == 0) lanes *= 2;
     const int direct = a.gs == lanes * VEC;
-    const int per_cta = tpr >= 128 || a.rows < 1024 ? 1 : 128 / tpr;
-    const size_t smem = direct ? 0 : (size_t)per_cta * a.G * sizeof(int);
-    return launch(rows_kernel<T, NORM, RES, VEC, NV>, dim3((unsigned)((a.rows + per_cta - 1) / per_cta)), tpr * per_cta, smem,
-                  stream, pdl, a, tpr, lanes, direct);
+    if (current_device(nullptr, &sms) != WFQ_OK) return cudaErrorInvalidDevice;
+    // short rows share a CTA of four warps where there are enough of them to go round
+    int per_cta = tpr >= 128 || a.rows < 8 * sms ? 1 : 128 / tpr;
+    const size_t row_smem = direct ? 0 : 2 * (size_t)a.G * sizeof(int);
+    while (per_cta > 1 && per_cta * row_smem > 40 * 1024) --per_cta;
+    const int ctas = (int)((a.rows + (long long)per_cta - 1) / per_cta), threads = tpr * per_cta;
+    auto kernel = rows_kernel<T, NORM, RES, VEC, NV, THREADS>;
+    static std::atomic<int> regs{0};       // of this kernel, looked up once
+    int r = regs.load(std::memory_order_relaxed);
+    if (r == 0) {
+        cudaFuncAttributes fa;
+        const cudaError_t err = cudaFuncGetAttributes(&fa, kernel);
+        if (err != cudaSuccess) return err;
+        r = fa.numRegs;
+        regs.store(r, std::memory_order_relaxed);
+    }
+    const int resident = resident_ctas(r, threads, per_cta * row_smem) * sms;      // as many as run at once
+    return launch(kernel, dim3((unsigned)(ctas < resident ? ctas : resident)), threads,
+                  per_cta * row_smem, stream, pdl, a, tpr, lanes, direct);
 }
 
-template <typename T, int VEC, int NV>
+template <typename T, int VEC, int NV, int THREADS>
 cudaError_t launch_rows_mode(const RowsArgs &a, int tpr, cudaStream_t stream, bool pdl)
 {
-    if (!a.gain) return launch_rows_kernel<T, false, false, VEC, NV>(a, tpr, stream, pdl);
-    if (!a.residual) return launch_rows_kernel<T, true, false, VEC, NV>(a, tpr, stream, pdl);
-    return launch_rows_kernel<T, true, true, VEC, NV>(a, tpr, stream, pdl);
+    if (!a.gain) return launch_rows_kernel<T, false, false, VEC, NV, THREADS>(a, tpr, stream, pdl);
+    if (!a.residual) return launch_rows_kernel<T, true, false, VEC, NV, THREADS>(a, tpr, stream, pdl);
+    return launch_rows_kernel<T, true, true, VEC, NV, THREADS>(a, tpr, stream, pdl);
+}
+template <typename T, int VEC, int NV>
+cudaError_t launch_rows_size(const RowsArgs &a, int tpr, cudaStream_t stream, bool pdl)
+{
+    return tpr <= 256 ? launch_rows_mode<T, VEC, NV, 256>(a, tpr, stream, pdl)
+                      : launch_rows_mode<T, VEC, NV, 1024>(a, tpr, stream, pdl);
 }
 
 bool aligned16(const void *p, long long ld, size_t elem)
@@ -344,17 +419,17 @@ cudaError_t launch_rows_t(const RowsArgs &a, cudaStream_t stream, bool pdl)
     const size_t e = sizeof(T);
     const bool wide = a.C % 8 == 0 && aligned16(a.x, a.ldx, e) && (!a.residual || aligned16(a.residual, a.ldr, e)) &&
                       (!a.h || aligned16(a.h, a.ldh, e)) && (!a.gain || aligned16(a.gain, 0, 4));
-    // elements per thread: 8 where that takes no more than 1024 threads and there are few rows, else 16 or 32
+    // Elements per thread: 8 where there are few rows (latency) or the elements are single or 32-bit loads, else 16; 32 for
+    // rows that would not fit a CTA otherwise.
+    const int want = !wide || e == 4 || a.rows < 592 ? 8 : 16;
     for (int per : {8, 16, 32}) {
-        const int tpr = (a.Cp / per + (a.Cp % per != 0) + 31) / 32 * 32;
-        if (tpr > 1024 || (per == 8 && a.rows > 592)) continue;
+        const int tpr = ((a.Cp + per - 1) / per + 31) / 32 * 32;
+        if (tpr > 1024 || per < want || a.G > 2048) continue;
         if (wide)
-            return per == 8 ? launch_rows_mode<T, 8, 1>(a, tpr, stream, pdl)
-                            : per == 16 ? launch_rows_mode<T, 8, 2>(a, tpr, stream, pdl)
-                                        : launch_rows_mode<T, 8, 4>(a, tpr, stream, pdl);
-        return per == 8 ? launch_rows_mode<T, 1, 8>(a, tpr, stream, pdl)
-                        : per == 16 ? launch_rows_mode<T, 1, 16>(a, tpr, stream, pdl)
-                                    : launch_rows_mode<T, 1, 32>(a, tpr, stream, pdl);
+            return per == 8 ? launch_rows_size<T, 8, 1>(a, tpr, stream, pdl)
+                            : per == 16 ? launch_rows_size<T, 8, 2>(a, tpr, stream, pdl)
+                                        : launch_rows_size<T, 8, 4>(a, tpr, stream, pdl);
+        if (per == 8) return launch_rows_size<T, 1, 8>(a, tpr, stream, pdl);
     }
     const int grid = a.rows < (1 << 20) ? a.rows : 1 << 20;
     const size_t smem = (size_t)a.G * sizeof(int);
