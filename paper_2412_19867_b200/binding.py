@@ -273,13 +273,15 @@ def wfq_rms_norm_quantize(x_dev, ldx, residual_dev, ldr, gain_dev, eps, dtype, r
 
 
 def wfq_quantize_rows(x_dev, ldx, dtype, rows, C, group_size, codes_dev, scales_dev, stream=0):
-    _check((_lib or load()).wfq_quantize_rows(x_dev, ldx, dtype, rows, C, group_size, codes_dev, scales_dev, stream),
-           "wfq_quantize_rows")
+    status = (_lib or load()).wfq_quantize_rows(x_dev, ldx, dtype, rows, C, group_size, codes_dev, scales_dev, stream)
+    if status != WFQ_OK:
+        _check(status, "wfq_quantize_rows")
 
 
 def wfq_dequantize_rows(codes_dev, scales_dev, rows, C, group_size, dtype, v_dev, ldv, stream=0):
-    _check((_lib or load()).wfq_dequantize_rows(codes_dev, scales_dev, rows, C, group_size, dtype, v_dev, ldv, stream),
-           "wfq_dequantize_rows")
+    status = (_lib or load()).wfq_dequantize_rows(codes_dev, scales_dev, rows, C, group_size, dtype, v_dev, ldv, stream)
+    if status != WFQ_OK:
+        _check(status, "wfq_dequantize_rows")
 
 
 def wfq_linear_create(C, K, group_size, gated=0):
@@ -495,24 +497,34 @@ class Conv:
 
 
 # ---- the operators around the convolutions --------------------------------------------
+# A decoding step's kernels take less than these calls: nothing in them that is not needed per call (queued, one row of
+# 4096: norm and dequantization 28 us with an import, a dict and two allocations more per call).
 
 _DTYPES = {"f32": WFQ_F32, "f16": WFQ_F16, "bf16": WFQ_BF16}
+_torch = None          # the module, and its types by the library's codes, once something here has been called
+_CODES = {}
+_NAMED = {}
 
 
-def _torch_dtypes():
+def _load_torch():
+    global _torch
     import torch
-    return {torch.float32: WFQ_F32, torch.float16: WFQ_F16, torch.bfloat16: WFQ_BF16}
+    _CODES.update({torch.float32: WFQ_F32, torch.float16: WFQ_F16, torch.bfloat16: WFQ_BF16})
+    _NAMED.update({"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16})
+    _torch = torch
+    return torch
 
 
 def _rows_of(x, C, what):
     """Rows and leading dimension of a tensor [..., C] whose rows lie one after another at one distance."""
-    assert x.is_cuda and x.dim() >= 1 and x.shape[-1] == C, what
+    shape = x.shape
+    assert x.is_cuda and shape and shape[-1] == C, what
     rows = x.numel() // C
     if x.is_contiguous() or rows == 0:
         return rows, C
     assert C == 1 or x.stride(-1) == 1, f"{what}: channels must be contiguous"
     ld, span = None, 1                   # distance between rows, rows that the dimensions behind this one hold
-    for size, stride in zip(reversed(x.shape[:-1]), reversed(x.stride()[:-1])):
+    for size, stride in zip(reversed(shape[:-1]), reversed(x.stride()[:-1])):
         if size != 1:
             if ld is None:
                 ld = stride
@@ -523,38 +535,49 @@ def _rows_of(x, C, what):
     return rows, max(ld, C)
 
 
+def _empty(shape, dtype, device):
+    strides, n = [], 1
+    for size in reversed(shape):
+        strides.append(n)
+        n *= size if size else 1
+    return _torch.empty_strided(shape, strides[::-1], dtype=dtype, device=device)
+
+
+def _call(index, fn, *args):
+    """fn(*args, stream) with device `index` current, on its current stream."""
+    c = _torch._C
+    if c._cuda_getDevice() == index:
+        fn(*args, c._cuda_getCurrentRawStream(index))
+    else:
+        with _torch.cuda.device(index):
+            fn(*args, c._cuda_getCurrentRawStream(index))
+
+
 class QuantizedRows:
-    """int8 codes [rows][Cp] and fp32 scales [G][Rs] of rows of C channels (layouts: include/wfq.h)."""
+    """int8 codes [rows][Cp] and fp32 scales [G][Rs] of rows of C channels (layouts: include/wfq.h) in one buffer."""
+    __slots__ = ("rows", "C", "group_size", "shape", "groups", "index", "_buf", "_codes", "_scales", "_at")
 
     def __init__(self, rows, C, group_size, device, shape=None):
-        import torch
+        if _torch is None:
+            _load_torch()
         self.rows, self.C, self.group_size = rows, C, group_size
-        self.shape = tuple(shape) if shape is not None else (rows, C)
-        groups = 1 if group_size == 0 or group_size >= C else -(-C // group_size)
-        self.codes = torch.empty((rows, (C + 31) // 32 * 32), dtype=torch.int8, device=device)
-        self.scales = torch.empty((groups, (rows + 127) // 128 * 128), dtype=torch.float32, device=device)
+        self.shape = (rows, C) if shape is None else shape
+        self.groups = 1 if group_size == 0 or group_size >= C else -(-C // group_size)
+        self._at = (rows * ((C + 31) // 32 * 32) + 255) // 256 * 256             # where the scales begin
+        self._buf = _torch.empty_strided((self._at + 4 * self.groups * ((rows + 127) // 128 * 128),), (1,),
+                                         dtype=_torch.int8, device=device)
+        self._codes = self._buf.data_ptr()
+        self._scales = self._codes + self._at
+        self.index = self._buf.get_device()
 
+    @property
+    def codes(self):
+        Cp = (self.C + 31) // 32 * 32
+        return self._buf[:self.rows * Cp].view(self.rows, Cp)
 
-class _on:
-    """The device of a tensor made current for a call, where it is not already; gives the current raw stream."""
-    __slots__ = ("guard", "index")
-
-    def __init__(self, device):
-        self.index = device.index
-
-    def __enter__(self):
-        import torch
-        here = torch._C._cuda_getDevice()
-        self.guard = None
-        if self.index is not None and self.index != here:
-            self.guard = torch.cuda.device(self.index)
-            self.guard.__enter__()
-            here = self.index
-        return torch._C._cuda_getCurrentRawStream(here)
-
-    def __exit__(self, *args):
-        if self.guard is not None:
-            self.guard.__exit__(*args)
+    @property
+    def scales(self):
+        return self._buf[self._at:].view(_torch.float32).view(self.groups, (self.rows + 127) // 128 * 128)
 
 
 def rms_norm_quantize(x, gain, eps=1e-6, group_size=128, residual=None, out=None):
@@ -562,50 +585,48 @@ def rms_norm_quantize(x, gain, eps=1e-6, group_size=128, residual=None, out=None
 
     x, residual: CUDA tensors [..., C] of one type (fp32, fp16, bf16); gain: fp32 [C].  h is the sum in x's type, written
     to `out` where given (residual itself is allowed); without a residual it is x."""
-    import torch
-    C = gain.numel()
-    dtypes = _torch_dtypes()
-    assert x.dtype in dtypes, "x: fp32, fp16 or bf16"
-    assert gain.is_cuda and gain.device == x.device and gain.dtype == torch.float32 and gain.is_contiguous()
+    torch = _torch or _load_torch()
+    C, dtype = gain.numel(), x.dtype
+    code, index = _CODES.get(dtype), x.get_device()
+    assert code is not None, "x: fp32, fp16 or bf16"
+    assert gain.dtype is torch.float32 and gain.get_device() == index and gain.is_contiguous(), "gain"
     rows, ldx = _rows_of(x, C, "x")
-    q = QuantizedRows(rows, C, group_size, x.device, x.shape)
-    h, ldr, ldh = None, 0, 0
-    if residual is not None:
-        assert residual.shape == x.shape and residual.dtype == x.dtype and residual.device == x.device
-        _, ldr = _rows_of(residual, C, "residual")
-        h = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-        assert h.shape == x.shape and h.dtype == x.dtype and h.device == x.device
-        _, ldh = _rows_of(h, C, "out")
-    else:
+    shape, device = x.shape, x.device
+    q = QuantizedRows(rows, C, group_size, device, shape)
+    if residual is None:
         assert out is None, "out: only with a residual"
-    with _on(x.device) as stream:
-        wfq_rms_norm_quantize(x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr, gain.data_ptr(),
-                              eps, dtypes[x.dtype], rows, C, group_size, None if h is None else h.data_ptr(), ldh,
-                              q.codes.data_ptr(), q.scales.data_ptr(), stream)
-    return q, x if h is None else h
+        _call(index, wfq_rms_norm_quantize, x.data_ptr(), ldx, None, 0, gain.data_ptr(), eps, code, rows, C, group_size,
+              None, 0, q._codes, q._scales)
+        return q, x
+    assert residual.shape == shape and residual.dtype is dtype and residual.get_device() == index, "residual"
+    _, ldr = _rows_of(residual, C, "residual")
+    if out is None:
+        h, ldh = _empty(shape, dtype, device), C
+    else:
+        h = out
+        assert h.shape == shape and h.dtype is dtype and h.get_device() == index, "out"
+        _, ldh = _rows_of(h, C, "out")
+    _call(index, wfq_rms_norm_quantize, x.data_ptr(), ldx, residual.data_ptr(), ldr, gain.data_ptr(), eps, code, rows, C,
+          group_size, h.data_ptr(), ldh, q._codes, q._scales)
+    return q, h
 
 
 def quantize_rows(x, group_size=128):
     """The rows of a CUDA tensor [..., C] as QuantizedRows."""
-    dtypes = _torch_dtypes()
-    assert x.dtype in dtypes, "x: fp32, fp16 or bf16"
-    C = x.shape[-1]
+    if _torch is None:
+        _load_torch()
+    code, C = _CODES.get(x.dtype), x.shape[-1]
+    assert code is not None, "x: fp32, fp16 or bf16"
     rows, ldx = _rows_of(x, C, "x")
     q = QuantizedRows(rows, C, group_size, x.device, x.shape)
-    with _on(x.device) as stream:
-        wfq_quantize_rows(x.data_ptr(), ldx, dtypes[x.dtype], rows, C, group_size, q.codes.data_ptr(),
-                          q.scales.data_ptr(), stream)
+    _call(q.index, wfq_quantize_rows, x.data_ptr(), ldx, code, rows, C, group_size, q._codes, q._scales)
     return q
 
 
 def dequantize_rows(q, dtype="f16"):
     """The values of QuantizedRows in "f32", "f16" or "bf16", shaped like the tensor they came from."""
-    import torch
-    v = torch.empty(q.shape, dtype={"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[dtype],
-                    device=q.codes.device)
-    with _on(v.device) as stream:
-        wfq_dequantize_rows(q.codes.data_ptr(), q.scales.data_ptr(), q.rows, q.C, q.group_size, _DTYPES[dtype],
-                            v.data_ptr(), q.C, stream)
+    v = _empty(q.shape, _NAMED[dtype], q._buf.device)
+    _call(q.index, wfq_dequantize_rows, q._codes, q._scales, q.rows, q.C, q.group_size, _DTYPES[dtype], v.data_ptr(), q.C)
     return v
 
 
@@ -613,77 +634,68 @@ class Linear:
     """A linear layer on group-wise int8 operands (include/wfq.h): C channels to K outputs, up to max_rows rows a call."""
 
     def __init__(self, C, K, group_size=128, max_rows=1, dtype="f16", out_dtype=None, gated=False, device="cuda:0"):
-        import torch
-        self.torch = torch
+        torch = _torch or _load_torch()
+        self.lin = None
         self.C, self.K, self.gs, self.gated = C, K, group_size, bool(gated)
         self.max_rows = max_rows
-        self.device = torch.device(device)
-        names = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
-        self._in, self._out = names[dtype], names[out_dtype or dtype]
+        self._in, self._out = _NAMED[dtype], _NAMED[out_dtype or dtype]
         self._bias = None
-        self.lin = None
         self.lin = wfq_linear_create(C, K, group_size, gated)
         wfq_linear_set_input_dtype(self.lin, _DTYPES[dtype])
         wfq_linear_set_output_dtype(self.lin, _DTYPES[out_dtype or dtype])
         nbytes = wfq_linear_workspace_bytes(self.lin, max_rows)
-        self._ws = torch.empty(nbytes + 1024, dtype=torch.uint8, device=self.device)
-        self.device = self._ws.device
-        with _on(self.device):
+        self._ws = torch.empty(nbytes + 1024, dtype=torch.uint8, device=device)
+        self.device, self.index = self._ws.device, self._ws.get_device()
+        with torch.cuda.device(self.index):
             wfq_linear_set_workspace(self.lin, (self._ws.data_ptr() + 1023) // 1024 * 1024, nbytes, max_rows)
 
     def prepare(self, w):
         """w: CUDA tensor [K][C] ([2K][C] if gated: gates, then values), fp32, fp16 or bf16."""
-        dtypes = _torch_dtypes()
-        assert w.device == self.device and w.dtype in dtypes
+        assert w.get_device() == self.index and w.dtype in _CODES
         assert w.shape == ((2 if self.gated else 1) * self.K, self.C)
         _, ldw = _rows_of(w, self.C, "w")
-        with _on(self.device) as stream:
-            wfq_linear_prepare_weights(self.lin, w.data_ptr(), ldw, dtypes[w.dtype], stream)
+        _call(self.index, wfq_linear_prepare_weights, self.lin, w.data_ptr(), ldw, _CODES[w.dtype])
 
     def set_epilogue(self, bias=None, act=WFQ_ACT_NONE):
         """bias: fp32 CUDA tensor [K] ([2K] if gated) or None; kept alive by this object."""
         if bias is not None:
-            assert bias.device == self.device and bias.dtype == self.torch.float32 and bias.is_contiguous()
+            assert bias.get_device() == self.index and bias.dtype is _torch.float32 and bias.is_contiguous()
             assert bias.numel() == (2 if self.gated else 1) * self.K
         wfq_linear_set_epilogue(self.lin, None if bias is None else bias.data_ptr(), act)
         self._bias = bias
 
-    def _outputs(self, lead, rows, residual, y):
-        shape = (*lead, self.K)
+    def _outputs(self, lead, residual, y):
+        K, shape = self.K, (*lead, self.K)
         if y is None:
-            y = self.torch.empty(shape, dtype=self._out, device=self.device)
-            ldy = self.K
+            y, ldy = _empty(shape, self._out, self.device), K
         else:
-            assert y.shape == shape and y.dtype is self._out and y.device == self.device
-            _, ldy = _rows_of(y, self.K, "y")
-        ldr = 0
-        if residual is not None:
-            assert residual.shape == shape and residual.dtype is self._out and residual.device == self.device
-            _, ldr = _rows_of(residual, self.K, "residual")
-        return y, ldy, None if residual is None else residual.data_ptr(), ldr
+            assert y.shape == shape and y.dtype is self._out and y.get_device() == self.index, "y"
+            _, ldy = _rows_of(y, K, "y")
+        if residual is None:
+            return y, ldy, None, 0
+        assert residual.shape == shape and residual.dtype is self._out and residual.get_device() == self.index, "residual"
+        _, ldr = _rows_of(residual, K, "residual")
+        return y, ldy, residual.data_ptr(), ldr
 
     def forward(self, x, residual=None, y=None):
         """x [..., C] -> y [..., K] (+ residual, which may be y)."""
-        assert x.dtype is self._in and x.device == self.device
+        assert x.dtype is self._in and x.get_device() == self.index, "x"
         rows, ldx = _rows_of(x, self.C, "x")
-        y, ldy, res, ldr = self._outputs(x.shape[:-1], rows, residual, y)
-        with _on(self.device) as stream:
-            wfq_linear_forward(self.lin, x.data_ptr(), ldx, rows, res, ldr, y.data_ptr(), ldy, stream)
+        y, ldy, res, ldr = self._outputs(x.shape[:-1], residual, y)
+        _call(self.index, wfq_linear_forward, self.lin, x.data_ptr(), ldx, rows, res, ldr, y.data_ptr(), ldy)
         return y
 
     def forward_codes(self, q, residual=None, y=None):
         """The same on QuantizedRows of C channels in this layer's groups."""
-        assert q.C == self.C and q.codes.device == self.device
-        assert q.group_size == self.gs or (len(q.scales) == 1 and (self.gs == 0 or self.gs >= self.C))
-        y, ldy, res, ldr = self._outputs(q.shape[:-1], q.rows, residual, y)
-        with _on(self.device) as stream:
-            wfq_linear_forward_codes(self.lin, q.codes.data_ptr(), q.scales.data_ptr(), q.rows, res, ldr, y.data_ptr(),
-                                     ldy, stream)
+        assert q.C == self.C and q.index == self.index, "q"
+        assert q.group_size == self.gs or (q.groups == 1 and (self.gs == 0 or self.gs >= self.C)), "q: groups"
+        y, ldy, res, ldr = self._outputs(q.shape[:-1], residual, y)
+        _call(self.index, wfq_linear_forward_codes, self.lin, q._codes, q._scales, q.rows, res, ldr, y.data_ptr(), ldy)
         return y
 
     def check_status(self):
-        with _on(self.device) as stream:
-            st, where = wfq_linear_check_status(self.lin, stream)
+        with _torch.cuda.device(self.index):
+            st, where = wfq_linear_check_status(self.lin, _torch._C._cuda_getCurrentRawStream(self.index))
         if st != WFQ_OK:
             raise WfqError(st, f"device status (wait id {where})")
 

@@ -42,6 +42,7 @@ struct wfq_linear {
     long long wait_cycles = 2000000000LL;
     int debug_skip_stage = -1;
     int debug_shape = 0;
+    int shape_rows = -1, shape_orient = 0, shape_bn = 0, shape_split = 0;   // what choose() said last, and for which rows
 };
 
 namespace wfq {
@@ -946,7 +947,11 @@ cudaError_t launch_variant(const wfq_linear &l, MmaArgs &a, int grid, const int8
 cudaError_t launch_product(wfq_linear &l, const int8_t *xq, const float *sx, int rows, const OutArgs &out,
                            cudaStream_t stream, bool pdl)
 {
-    const Shape sp = choose(l, rows);
+    if (l.shape_rows != rows) {
+        const Shape s = choose(l, rows);
+        l.shape_rows = rows; l.shape_orient = s.orient; l.shape_bn = s.bn; l.shape_split = s.split;
+    }
+    const Shape sp{l.shape_orient, l.shape_bn, l.shape_split};
     MmaArgs a;
     const long long sx_pitch = (rows + 127LL) / 128 * 128;
     const bool swap = sp.orient == 2, pair = sp.orient == 3;
@@ -1202,6 +1207,7 @@ wfq_status_t wfq_linear_set_debug_option(wfq_linear_t *l, wfq_debug_option_t opt
             if (value != 0 && (value < 0 || value > 99999 || !parts || !known_shape(sp) || (l->Cp + 127) / 128 < sp.split))
                 return WFQ_ERR_INVALID_ARG;
             l->debug_shape = (int)value;
+            l->shape_rows = -1;
             return WFQ_OK;
         }
         default: return WFQ_ERR_INVALID_ARG;
