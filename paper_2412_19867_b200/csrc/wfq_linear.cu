@@ -7,9 +7,9 @@
 // work).  With PAIR two CTAs share a tile of 256 rows (tcgen05.mma.cta_group::2): each loads its 128 rows and half of the
 // columns' operand.  Gated weights are stored with gate and value channels alternating, so that a pair is two neighbours.
 //   warp 0      TMA producer: 128 channels of both operands per stage (128-byte swizzle)
-//   warp 1      allocates TMEM, issues tcgen05.mma kind::i8 (K = 32): a piece is a group, or up to 256 channels of a longer
-//               one, as far as this CTA has them; pieces of a chunk (up to 128 channels where the group divides 128) lie
-//               side by side in one TMEM slot
+//   warp 1      allocates TMEM, issues tcgen05.mma kind::i8 (K = 32): a piece is a group, as far as this CTA has its
+//               channels; pieces of a chunk (up to 128 channels where the group divides 128) lie side by side in one TMEM
+//               slot
 //   warp 2      scale loader: 128 row scales and BN column scales per piece
 //   warps 4-11  epilogue: int32 sums to fp32, times the scales, into registers; then bias, activation, gate, residual
 // With few tiles a cluster of up to eight CTAs shares one: each takes a range of the channels, the partial sums are
@@ -114,7 +114,6 @@ struct MmaArgs {
     int tiles, MT;             // tiles, blocks of 128 (PAIR: 256) rows
     int split;                 // CTAs that share the channels of a tile (cluster size; 1 with PAIR)
     int steps, gsteps, cg;     // MMA steps of 32 channels in all, per group; pieces per chunk (as in issue())
-    int ppg;                   // pieces per group
     int *status;
     long long wait_cycles;
     int debug_skip_stage;
@@ -122,14 +121,8 @@ struct MmaArgs {
     OutArgs out;
 };
 
-// The channels of this CTA: stages, steps and pieces.  A group's pieces are PIECE steps long but the last one, wherever
-// the CTAs' ranges begin.
-constexpr int PIECE = 8;
-struct Range { int kb0, kb1, s0, s1, p0, np; };
-__device__ __forceinline__ int piece_of(const MmaArgs &a, int step)
-{
-    return step / a.gsteps * a.ppg + step % a.gsteps / PIECE;
-}
+// The channels of this CTA: stages, steps and the pieces (groups, or parts of them) that they fall into.
+struct Range { int kb0, kb1, s0, s1, g0, np; };
 __device__ __forceinline__ Range range_of(const MmaArgs &a, int rank)
 {
     Range r;
@@ -138,8 +131,8 @@ __device__ __forceinline__ Range range_of(const MmaArgs &a, int rank)
     r.kb1 = (int)((long long)KB * (rank + 1) / a.split);
     r.s0 = 4 * r.kb0;
     r.s1 = min(a.steps, 4 * r.kb1);
-    r.p0 = piece_of(a, r.s0);
-    r.np = piece_of(a, r.s1 - 1) - r.p0 + 1;
+    r.g0 = r.s0 / a.gsteps;
+    r.np = (r.s1 - 1) / a.gsteps - r.g0 + 1;
     return r;
 }
 
@@ -580,7 +573,7 @@ __device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tm
             if constexpr (GST == 4) {
                 if (begins && !wait<C>(free0 + 8u * slot, sphase ^ 1u, ctx, kWaitTmemEmpty)) return;
                 in_group += n;
-                const bool ends = in_group == a.gsteps || in_group % PIECE == 0 || 4 * kb + n == rg.s1;
+                const bool ends = in_group == a.gsteps || 4 * kb + n == rg.s1;
                 ptx::tc_fence_after();
                 if (ptx::elect_one()) {
                     const uint32_t d = tmem_base + (uint32_t)(slot * SLOT_COLS);
@@ -626,7 +619,7 @@ __device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tm
                         if (!wait<C>(free0 + 8u * slot, sphase ^ 1u, ctx, kWaitTmemEmpty)) return;
                         ptx::tc_fence_after();
                     }
-                    const bool ends = ++in_group == a.gsteps || in_group % PIECE == 0 || 4 * kb + s + 1 == rg.s1;
+                    const bool ends = ++in_group == a.gsteps || 4 * kb + s + 1 == rg.s1;
                     if (ptx::elect_one()) {
                         const uint32_t d = tmem_base + (uint32_t)(slot * SLOT_COLS);
                         mma(d, a_lo + 2 * s, b_lo + 2 * s, begins);
@@ -770,7 +763,7 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                 __syncwarp();
                 if (lane < 8 && (lane & 3) < n) {      // lane j: row scales of piece j, lane 4 + j: column scales
                     const int j = lane & 3;
-                    const long long g = (rg.p0 + q0 + j) / a.ppg;
+                    const long long g = rg.g0 + q0 + j;
                     const uint32_t d = dst + (uint32_t)(j * C::GROUP_SCALE_FLOATS * 4);
                     if (lane < 4) ptx::bulk_load(d, a.row_scale + g * a.row_pitch + row0, BM * 4, bar);
                     else ptx::bulk_load(d + BM * 4, a.col_scale + g * a.col_pitch + nt * BN, BN * 4, bar);
@@ -966,7 +959,6 @@ cudaError_t launch_product(wfq_linear &l, const int8_t *xq, const float *sx, int
     a.split = sp.split;
     a.steps = l.Cp / UK;
     a.gsteps = l.gs / UK;
-    a.ppg = (a.gsteps + PIECE - 1) / PIECE;
     a.status = l.status;
     a.wait_cycles = l.wait_cycles;
     a.debug_skip_stage = l.debug_skip_stage;
