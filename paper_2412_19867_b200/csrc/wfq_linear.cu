@@ -52,9 +52,8 @@ namespace {
 constexpr int BM = 128;
 constexpr int BK = 128;
 constexpr int UK = 32;
-constexpr int NSLOT = 2;
-constexpr int SLOT_COLS = 256;
-constexpr int TMEM_COLS = NSLOT * SLOT_COLS;
+constexpr int TMEM_COLS = 512;
+constexpr int MAX_SLOTS = 16;
 constexpr int A_BYTES = BM * BK;
 constexpr int EPI_WARPS = 8;
 constexpr int FIRST_EPI_WARP = 4;
@@ -63,8 +62,8 @@ constexpr int THREADS = 32 * (FIRST_EPI_WARP + EPI_WARPS);
 
 struct Shared {
     uint64_t full[16], empty[16];
-    uint64_t acc_full[NSLOT], slot_free[NSLOT];
-    uint64_t scale_free[NSLOT];      // PAIR: this CTA's epilogue is done with a slot (slot_free counts both CTAs')
+    uint64_t acc_full[MAX_SLOTS], slot_free[MAX_SLOTS];
+    uint64_t scale_free[MAX_SLOTS];  // PAIR: this CTA's epilogue is done with a slot (slot_free counts both CTAs')
     uint64_t mma_done;
     uint32_t tmem_base;
     volatile int abort;
@@ -75,13 +74,16 @@ struct Cfg {
     static_assert(!(SWAP && PAIR), "pairs: rows of x on the lanes");
     static constexpr int B_ROWS = PAIR ? BN / 2 : BN;             // of the columns' operand in this CTA
     static constexpr int STAGE_BYTES = A_BYTES + B_ROWS * BK;
-    static constexpr int STAGES = STAGE_BYTES > 24 * 1024 ? 5 : STAGE_BYTES > 20 * 1024 ? (SWAP ? 8 : 7) : 10;
+    static constexpr int STAGES = STAGE_BYTES > 24 * 1024 ? 5 : STAGE_BYTES > 20 * 1024 ? (SWAP ? 8 : 7) : 9;
     static constexpr int PATCH_BYTES = SWAP ? 0 : 32 * PATCH_PITCH * 4;           // of one epilogue warp
-    static constexpr int CG_MAX = SLOT_COLS / BN < 4 ? SLOT_COLS / BN : 4;        // pieces per chunk at most
+    // Pieces in tensor memory at a time, with their scales: chunks of one (of up to CG_MAX short groups) in as many slots
+    // as that gives.  The scales of a slot are asked for when it is free; with two slots whatever the number of columns
+    // that took longer than a stage of weights (24 rows, 4096 -> 16384 gated: 0.6 us per 128 channels).
+    static constexpr int PIECES = 512 / BN < 16 ? 512 / BN : 16;
+    static constexpr int CG_MAX = PIECES / 2 < 4 ? PIECES / 2 : 4;
     static constexpr int GROUP_SCALE_FLOATS = BM + BN;
-    static constexpr int SLOT_SCALE_FLOATS = CG_MAX * GROUP_SCALE_FLOATS;
     static constexpr size_t SMEM_BYTES = 1024 + (size_t)STAGES * STAGE_BYTES + EPI_WARPS * PATCH_BYTES +
-                                         (size_t)NSLOT * SLOT_SCALE_FLOATS * 4 + sizeof(Shared);
+                                         (size_t)PIECES * GROUP_SCALE_FLOATS * 4 + sizeof(Shared);
     static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
     static_assert(PAIR || (size_t)BN * (BM + 1) * 4 <= (size_t)STAGES * STAGE_BYTES, "partial sums fit the stages");
     // Registers behind setmaxnreg: the epilogue holds BN / 2 sums and two blocks of loads.
@@ -114,6 +116,7 @@ struct MmaArgs {
     int tiles, MT;             // tiles, blocks of 128 (PAIR: 256) rows
     int split;                 // CTAs that share the channels of a tile (cluster size; 1 with PAIR)
     int steps, gsteps, cg;     // MMA steps of 32 channels in all, per group; pieces per chunk (as in issue())
+    int slots;                 // chunks in tensor memory
     int *status;
     long long wait_cycles;
     int debug_skip_stage;
@@ -479,14 +482,17 @@ __device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, cons
     const bool active = row0 + quarter * 32 < a.rows && col0 + ec.c0 < a.cols;
     Sums<CW, SWAP> sums;
     sums.zero();
+    bool ready = false;              // the slot was seen to be full ahead of its turn
     for (int q0 = 0; q0 < rg.np; q0 += a.cg) {
         const int n = min(a.cg, rg.np - q0);
-        if (!wait<C>(ptx::smem_u32(&sh->acc_full[slot]), sphase, ctx, kWaitTmemFull)) return false;
+        if (!__all_sync(0xffffffffu, ready) &&
+            !wait<C>(ptx::smem_u32(&sh->acc_full[slot]), sphase, ctx, kWaitTmemFull))
+            return false;
         if (active) {
             ptx::tc_fence_after();
-            const float *sc = ec.scales + (size_t)slot * C::SLOT_SCALE_FLOATS;
+            const float *sc = ec.scales + (size_t)slot * a.cg * C::GROUP_SCALE_FLOATS;
             for (int j = 0; j < n; ++j) {
-                const uint32_t taddr = ec.tmem + (uint32_t)(slot * SLOT_COLS + j * BN);
+                const uint32_t taddr = ec.tmem + (uint32_t)((slot * a.cg + j) * BN);
                 const float *rows = sc + j * C::GROUP_SCALE_FLOATS + quarter * 32;
                 const float *cs = sc + j * C::GROUP_SCALE_FLOATS + BM + ec.c0;
                 if constexpr (SWAP) {
@@ -500,6 +506,11 @@ __device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, cons
             }
             ptx::tc_fence_before();
         }
+        if constexpr (BN >= 128) {       // wide tiles: a wait on a full slot is 10 % of a piece (2000 x 8192 -> 2048, groups of
+                                         // 128: 64.8 -> 61.3 us; with 64 columns 2 % slower)
+            const int after = slot + 1 == a.slots ? 0 : slot + 1;
+            ready = ptx::mbar_test_wait(ptx::smem_u32(&sh->acc_full[after]), after ? sphase : sphase ^ 1u);
+        }
         __syncwarp();
         if (ptx::elect_one()) {
             if constexpr (PAIR) {
@@ -510,7 +521,7 @@ __device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, cons
             }
         }
         __syncwarp();
-        if (++slot == NSLOT) { slot = 0; sphase ^= 1u; }
+        if (++slot == a.slots) { slot = 0; sphase ^= 1u; }
     }
     if constexpr (!PAIR) {
         if (a.split > 1) {           // [column][lane of TMEM], one float of padding per column
@@ -576,7 +587,7 @@ __device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tm
                 const bool ends = in_group == a.gsteps || 4 * kb + n == rg.s1;
                 ptx::tc_fence_after();
                 if (ptx::elect_one()) {
-                    const uint32_t d = tmem_base + (uint32_t)(slot * SLOT_COLS);
+                    const uint32_t d = tmem_base + (uint32_t)(slot * CG * BN);
                     mma(d, a_lo, b_lo, begins);
                     if (n > 1) mma(d, a_lo + 2, b_lo + 2, false);
                     if (n > 2) mma(d, a_lo + 4, b_lo + 4, false);
@@ -588,7 +599,7 @@ __device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tm
                 begins = ends;
                 if (in_group == a.gsteps) in_group = 0;
                 if (ends) {
-                    if (++slot == NSLOT) { slot = 0; sphase ^= 1u; }
+                    if (++slot == a.slots) { slot = 0; sphase ^= 1u; }
                 }
             } else if constexpr (GST > 0) {
 #pragma unroll
@@ -597,7 +608,7 @@ __device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tm
                         if (!wait<C>(free0 + 8u * slot, sphase ^ 1u, ctx, kWaitTmemEmpty)) return;
                         ptx::tc_fence_after();
                         if (ptx::elect_one()) {
-                            const uint32_t d = tmem_base + (uint32_t)(slot * SLOT_COLS);
+                            const uint32_t d = tmem_base + (uint32_t)(slot * CG * BN);
 #pragma unroll
                             for (int s = c; s < c + CG * GST; ++s)
                                 if (s < n) {
@@ -607,7 +618,7 @@ __device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tm
                             commit(acc0 + 8u * slot);
                         }
                         __syncwarp();
-                        if (++slot == NSLOT) { slot = 0; sphase ^= 1u; }
+                        if (++slot == a.slots) { slot = 0; sphase ^= 1u; }
                     }
                 }
                 if (ptx::elect_one()) commit(empty0 + 8u * stage);
@@ -621,7 +632,7 @@ __device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tm
                     }
                     const bool ends = ++in_group == a.gsteps || 4 * kb + s + 1 == rg.s1;
                     if (ptx::elect_one()) {
-                        const uint32_t d = tmem_base + (uint32_t)(slot * SLOT_COLS);
+                        const uint32_t d = tmem_base + (uint32_t)(slot * CG * BN);
                         mma(d, a_lo + 2 * s, b_lo + 2 * s, begins);
                         if (ends) commit(acc0 + 8u * slot);
                     }
@@ -629,7 +640,7 @@ __device__ __forceinline__ void issue(Shared *sh, uint32_t tiles_lo, uint32_t tm
                     begins = ends;
                     if (in_group == a.gsteps) in_group = 0;
                     if (ends) {
-                        if (++slot == NSLOT) { slot = 0; sphase ^= 1u; }
+                        if (++slot == a.slots) { slot = 0; sphase ^= 1u; }
                     }
                 }
                 if (ptx::elect_one()) commit(empty0 + 8u * stage);
@@ -649,7 +660,7 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     unsigned char *tiles = ptx::align_smem<1024>(smem_raw);
     float *patches = reinterpret_cast<float *>(tiles + (size_t)C::STAGES * C::STAGE_BYTES);
     float *scales = patches + EPI_WARPS * (C::PATCH_BYTES / 4);
-    Shared *sh = reinterpret_cast<Shared *>(scales + (size_t)NSLOT * C::SLOT_SCALE_FLOATS);
+    Shared *sh = reinterpret_cast<Shared *>(scales + (size_t)C::PIECES * C::GROUP_SCALE_FLOATS);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int ctas = PAIR ? 2 : a.split;                                   // of a cluster
     const int rank = (int)blockIdx.x % ctas, first = (int)blockIdx.x / ctas, stride = (int)gridDim.x / ctas;
@@ -662,7 +673,7 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             ptx::mbar_init(ptx::smem_u32(&sh->full[s]), 1);
             ptx::mbar_init(ptx::smem_u32(&sh->empty[s]), 1);
         }
-        for (int s = 0; s < NSLOT; ++s) {
+        for (int s = 0; s < MAX_SLOTS; ++s) {
             ptx::mbar_init(ptx::smem_u32(&sh->acc_full[s]), 2);       // MMAs, scales
             ptx::mbar_init(ptx::smem_u32(&sh->slot_free[s]), (PAIR ? 2 : 1) * EPI_WARPS);
             ptx::mbar_init(ptx::smem_u32(&sh->scale_free[s]), EPI_WARPS);
@@ -758,7 +769,7 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                 ok = wait<C>(scale_bar + 8u * slot, sphase ^ 1u, ctx, kWaitScaleEmpty);
                 if (!ok) break;
                 const uint32_t bar = ptx::smem_u32(&sh->acc_full[slot]);
-                const uint32_t dst = ptx::smem_u32(scales + (size_t)slot * C::SLOT_SCALE_FLOATS);
+                const uint32_t dst = ptx::smem_u32(scales + (size_t)slot * a.cg * C::GROUP_SCALE_FLOATS);
                 if (ptx::elect_one()) ptx::mbar_arrive_expect_tx(bar, (uint32_t)(n * C::GROUP_SCALE_FLOATS * 4));
                 __syncwarp();
                 if (lane < 8 && (lane & 3) < n) {      // lane j: row scales of piece j, lane 4 + j: column scales
@@ -770,15 +781,15 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                 }
                 __syncwarp();
                 ++issued;
-                if (++slot == NSLOT) { slot = 0; sphase ^= 1u; }
+                if (++slot == a.slots) { slot = 0; sphase ^= 1u; }
             }
         }
         if (!ok || sh->abort) {
             int s = slot;
             uint32_t ph = sphase;
-            const long long n = issued < NSLOT ? issued : NSLOT;
+            const long long n = issued < a.slots ? issued : a.slots;
             for (long long i = 0; i < n; ++i) {
-                if (--s < 0) { s = NSLOT - 1; ph ^= 1u; }
+                if (--s < 0) { s = a.slots - 1; ph ^= 1u; }
                 drain(ptx::smem_u32(&sh->acc_full[s]), ph);
             }
         }
@@ -863,6 +874,15 @@ bool known_shape(const Shape &s)
     return s.orient == 3 && s.split == 1 && (s.bn == 128 || s.bn == 256);
 }
 
+// Microseconds of a tile, from sweeps over the shapes below (rows 1 to 8192, groups of 32 to 128 and whole rows): a stage
+// of 128 channels takes its copies and MMAs or the promotion of its chunks, whichever is longer; then the results' way out.
+struct TileTime { double stage, chunk, piece, out; };
+TileTime tile_time(const Shape &s)
+{
+    if (s.orient == 2) return s.bn == 16 ? TileTime{.27, .2, .03, .3} : s.bn == 32 ? TileTime{.29, .2, .06, .4} : TileTime{.34, .2, .2, .8};
+    return s.bn == 64 ? TileTime{.25, .33, .05, 1.2} : s.bn == 128 ? TileTime{.26, .2, .3, 1.8} : TileTime{.37, .25, .62, 3.};
+}
+
 Shape choose(const wfq_linear &l, int rows)
 {
     if (l.debug_shape) return Shape{l.debug_shape / 1000 % 10, l.debug_shape % 1000, l.debug_shape / 10000};
@@ -878,14 +898,14 @@ Shape choose(const wfq_linear &l, int rows)
                 const int r = orient == 2 ? l.Kz : rows, c = orient == 2 ? rows : l.Kz;
                 const double tiles = (double)((r + lanes - 1) / lanes) * ((c + bn - 1) / bn);
                 if (split > 1 && (tiles * split > l.sm_count || KB < 2 * split)) continue;
-                const double per_piece = BM * bn / 45.0 + 200.0;
-                const double pieces = l.gs < 256 ? 128.0 / l.gs : 0.5;
-                double per_stage = pieces * per_piece;
-                const double bytes = (BM + (orient == 3 ? bn / 2 : bn)) * 128.0;
-                if (per_stage < bytes / 50.0) per_stage = bytes / 50.0;
+                const TileTime t = tile_time(sp);
+                const int pieces = 512 / bn < 16 ? 512 / bn : 16, cg_max = pieces / 2 < 4 ? pieces / 2 : 4;
+                const int cg = BK % l.gs != 0 ? 1 : BK / l.gs < cg_max ? BK / l.gs : cg_max;
+                double stage = 128.0 / l.gs / cg * (t.chunk + t.piece * cg);
+                if (stage < t.stage) stage = t.stage;
                 const int at_once = l.sm_count / per_tile;
                 const double waves = (double)(long long)((tiles + at_once - 1) / at_once);
-                const double cost = waves * (((KB + split - 1) / split) * per_stage + BM * bn / 8.0) + (split > 1 ? 2000.0 : 0.0);
+                const double cost = waves * ((KB + split - 1) / split * stage + t.out) + (split > 1 ? .8 : 0.);
                 if (cost < best_cost) { best_cost = cost; best = sp; }
             }
     return best;
@@ -912,6 +932,7 @@ cudaError_t launch_variant(const wfq_linear &l, MmaArgs &a, int grid, const int8
 {
     a.cg = 1;
     if (BK % l.gs == 0) a.cg = BK / l.gs < Cfg<BN, SWAP, PAIR>::CG_MAX ? BK / l.gs : Cfg<BN, SWAP, PAIR>::CG_MAX;
+    a.slots = Cfg<BN, SWAP, PAIR>::PIECES / a.cg;
     CUtensorMap tx, tw;
     if (!encode_codes(&tx, xq, l.Cp, rows, SWAP ? BN : BM) || !encode_codes(&tw, l.Wq, l.Cp, l.Kz, SWAP ? BM : Cfg<BN, SWAP, PAIR>::B_ROWS))
         return cudaErrorInvalidValue;
