@@ -50,20 +50,36 @@ template <typename T> __device__ __forceinline__ void store8(T *p, const float (
     }
 }
 
-// Scale and reciprocal of a group from the bit pattern of its largest magnitude.  A group that holds an infinity or a
-// NaN has the scale NaN and codes 0, so that what is computed from it is NaN.
-__device__ __forceinline__ void scale_of(int amax_bits, float &scale, float &inv)
+// Scale amax / 127 and reciprocal 127 / amax of a group, both correctly rounded: a quotient from an approximate reciprocal
+// is corrected by its remainder (Markstein's method), which gives the bits of __fdiv_rn for every float from 1e-30 to the
+// largest in a fraction of the instructions.  A group that holds an infinity or a NaN has the scale NaN and codes 0, so that
+// what is computed from it is NaN; inv is 0 where the codes are.
+__device__ __forceinline__ void scale_of(float amax, float &scale, float &inv)
 {
-    const float amax = __int_as_float(amax_bits);
-    const bool some = amax_bits < kNonFinite && amax >= 1e-30f;
-    scale = some ? __fdiv_rn(amax, 127.f) : amax_bits >= kNonFinite ? __int_as_float(0x7fc00000) : 0.f;
-    inv = some ? __fdiv_rn(127.f, amax) : 0.f;
+    constexpr float r127 = 1.f / 127.f;
+    float q = __fmul_rn(amax, r127);
+    scale = fmaf(fmaf(-127.f, q, amax), r127, q);
+    float r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(amax));
+    r = fmaf(r, fmaf(-amax, r, 1.f), r);
+    q = __fmul_rn(127.f, r);
+    inv = fmaf(fmaf(-amax, q, 127.f), r, q);
+    if (!(amax >= 1e-30f)) scale = inv = 0.f;
+    if (!(amax < __int_as_float(kNonFinite))) { scale = __int_as_float(0x7fc00000); inv = 0.f; }
 }
 __device__ __forceinline__ uint32_t code_bits(float u, float inv)
 {
     // product and sum rounded separately, as the quantizer is defined; the low byte of the sum is the code
     return __float_as_uint(__fadd_rn(__fmul_rn(u, inv), 12582912.f));
 }
+// The larger magnitude; NaN where one of the two is.
+__device__ __forceinline__ float larger(float m, float u)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(m), "f"(fabsf(u)));
+    return r;
+}
+// Magnitudes as integers are ordered as the numbers are, with infinity and NaN above them.
 __device__ __forceinline__ int magnitude_bits(float u) { return __float_as_int(u) & 0x7fffffff; }
 
 __device__ __forceinline__ int target_row(const RowsArgs &a, int row)
@@ -125,13 +141,13 @@ __global__ void __launch_bounds__(256) rows_any_kernel(RowsArgs a)
         const int to = target_row(a, row);
         for (int g = threadIdx.x; g < a.G; g += 256) {
             float scale, inv;
-            scale_of(group_max[g], scale, inv);
+            scale_of(__int_as_float(group_max[g]), scale, inv);
             a.scales[(size_t)g * a.scale_pitch + to] = NORM ? __fmul_rn(scale, rstd) : scale;
         }
         for (int c0 = warp * 32; c0 < a.Cp; c0 += 256) {
             const int c = c0 + lane;
             float scale, inv;
-            scale_of(group_max[c0 / a.gs], scale, inv);
+            scale_of(__int_as_float(group_max[c0 / a.gs]), scale, inv);
             uint32_t code = 0;
             if (c < a.C && inv > 0.f) {
                 float u = value(c, true);
@@ -205,12 +221,17 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? 3 
     };
     long long row = (long long)blockIdx.x * per_cta + local;
     ask(row);
-    if constexpr (NORM) {
+    // what a thread's vectors are to every row: their group, and whether they begin it
+    int group[NV];
+    float *to_scale[NV];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int v = i * tpr + t;
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * tpr + t) * VEC;
+        group[i] = c / a.gs;
+        to_scale[i] = c < a.C && c == group[i] * a.gs ? a.scales + (size_t)group[i] * a.scale_pitch : nullptr;
+        if constexpr (NORM) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) gain[i][e] = v < n ? __ldg(a.gain + v * VEC + e) : 0.f;
+            for (int e = 0; e < VEC; ++e) gain[i][e] = c < a.C ? __ldg(a.gain + c + e) : 0.f;
         }
     }
     for (long long k = 0; k < rounds; ++k, row += step) {
@@ -223,12 +244,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? 3 
         for (int i = 0; i < NV; ++i) {
             const bool has = live && i * tpr + t < n;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                float h = has ? x[i].get(e) : 0.f;
-                if constexpr (RES) {
-                    if (has) h = Elem<T>::get(Elem<T>::put(__fadd_rn(h, r[i].get(e))));
+            for (int e = 0; e < VEC; ++e) u[i][e] = 0.f;
+            if (has) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    u[i][e] = x[i].get(e);
+                    if constexpr (RES) u[i][e] = Elem<T>::get(Elem<T>::put(__fadd_rn(u[i][e], r[i].get(e))));
                 }
-                u[i][e] = h;
             }
         }
         ask(row + step);
@@ -249,12 +271,21 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? 3 
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) u[i][e] = __fmul_rn(u[i][e], gain[i][e]);
             }
-            amax[i] = 0;
+            float m = fabsf(u[i][0]);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) amax[i] = max(amax[i], magnitude_bits(u[i][e]));
-            for (int o = 1; o < lanes; o <<= 1) amax[i] = max(amax[i], __shfl_xor_sync(0xffffffffu, amax[i], o));
-            const int v = i * tpr + t;
-            if (!direct && v < n && (lane & (lanes - 1)) == 0) atomicMax(&gmax[v * VEC / a.gs], amax[i]);
+            for (int e = 1; e < VEC; ++e) m = larger(m, u[i][e]);
+            amax[i] = magnitude_bits(m);
+        }
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1)
+            if (o < lanes) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) amax[i] = max(amax[i], __shfl_xor_sync(0xffffffffu, amax[i], o));
+            }
+        if (!direct && (lane & (lanes - 1)) == 0) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (i * tpr + t < n) atomicMax(&gmax[group[i]], amax[i]);
         }
         if constexpr (NORM) {
 #pragma unroll
@@ -265,8 +296,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? 3 
         float rstd = 1.f;
         if constexpr (NORM) {
             if (tpr > 32) {
-                sum = 0.f;
-                for (int w = 0; w < tpr / 32; ++w) sum += warp_sum[odd][local * (tpr / 32) + w];
+                const int warps = tpr >> 5;
+                sum = lane < warps ? warp_sum[odd][local * warps + lane] : 0.f;
+#pragma unroll
+                for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
             }
             rstd = rstd_of(sum, a);
         }
@@ -281,19 +314,19 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? 3 
             for (int i = 0; i < NV; ++i) {
                 const int v = i * tpr + t;
                 if (v < a.Cp / VEC) {
-                    const int g = v * VEC / a.gs;
                     float scale, inv;
-                    scale_of(direct ? amax[i] : gmax[g], scale, inv);
-                    if (v * VEC == g * a.gs) a.scales[(size_t)g * a.scale_pitch + to] = NORM ? __fmul_rn(scale, rstd) : scale;
+                    scale_of(__int_as_float(direct || v >= n ? amax[i] : gmax[group[i]]), scale, inv);
+                    if (to_scale[i]) to_scale[i][to] = NORM ? __fmul_rn(scale, rstd) : scale;
                     uint32_t w[VEC];
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) w[e] = inv > 0.f ? code_bits(u[i][e], inv) : 0u;
+                    for (int e = 0; e < VEC; ++e) w[e] = code_bits(u[i][e], inv);
                     if constexpr (VEC == 8) {
-                        const uint32_t lo = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
-                        const uint32_t hi = __byte_perm(__byte_perm(w[4], w[5], 0x0040), __byte_perm(w[6], w[7], 0x0040), 0x5410);
+                        uint32_t lo = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
+                        uint32_t hi = __byte_perm(__byte_perm(w[4], w[5], 0x0040), __byte_perm(w[6], w[7], 0x0040), 0x5410);
+                        if (!(inv > 0.f)) lo = hi = 0;
                         *reinterpret_cast<uint2 *>(codes + v * 8) = make_uint2(lo, hi);
                     } else {
-                        codes[v] = (int8_t)w[0];
+                        codes[v] = inv > 0.f ? (int8_t)w[0] : (int8_t)0;
                     }
                 }
             }
