@@ -88,7 +88,7 @@ __device__ __forceinline__ int target_row(const RowsArgs &a, int row)
 }
 __device__ __forceinline__ float rstd_of(float sum, const RowsArgs &a)
 {
-    return __fdiv_rn(1.f, __fsqrt_rn(__fadd_rn(__fdiv_rn(sum, (float)a.C), a.eps)));
+    return rsqrtf(fmaf(sum, a.per_C, a.eps));      // two units in the last place, and the rounding of 1 / C
 }
 
 // Rows that registers do not hold.  One CTA per row, two passes over it; the second
@@ -160,6 +160,27 @@ __global__ void __launch_bounds__(256) rows_any_kernel(RowsArgs a)
     }
 }
 
+// a += b for eight elements, each sum rounded once.  A 16-bit sum rounded from 32 bits is the same: where 32 bits do not
+// hold it exactly the smaller term is less than a quarter of a step of the larger.
+__device__ __forceinline__ void add_words(float *a, const float *b)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] = __fadd_rn(a[i], b[i]);
+}
+__device__ __forceinline__ void add_words(__half *a, const __half *b)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        reinterpret_cast<__half2 *>(a)[i] = __hadd2(reinterpret_cast<__half2 *>(a)[i], reinterpret_cast<const __half2 *>(b)[i]);
+}
+__device__ __forceinline__ void add_words(__nv_bfloat16 *a, const __nv_bfloat16 *b)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        reinterpret_cast<__nv_bfloat162 *>(a)[i] =
+            __hadd2(reinterpret_cast<__nv_bfloat162 *>(a)[i], reinterpret_cast<const __nv_bfloat162 *>(b)[i]);
+}
+
 // VEC consecutive elements as they lie in memory (VEC 8: 16-byte aligned).
 template <typename T, int VEC> struct Raw {
     uint4 q[sizeof(T) / 2];
@@ -169,12 +190,25 @@ template <typename T, int VEC> struct Raw {
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) q[i] = src[i];
     }
+    __device__ __forceinline__ void put(T *p) const
+    {
+        uint4 *dst = reinterpret_cast<uint4 *>(p);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) dst[i] = q[i];
+    }
     __device__ __forceinline__ float get(int e) const { return Elem<T>::get(reinterpret_cast<const T *>(q)[e]); }
+    __device__ __forceinline__ void add(const Raw &o) { add_words(reinterpret_cast<T *>(q), reinterpret_cast<const T *>(o.q)); }
 };
 template <typename T> struct Raw<T, 1> {
     T v;
     __device__ __forceinline__ void load(const T *p) { v = *p; }
+    __device__ __forceinline__ void put(T *p) const { *p = v; }
     __device__ __forceinline__ float get(int) const { return Elem<T>::get(v); }
+    __device__ __forceinline__ void add(const Raw &o)
+    {
+        if constexpr (sizeof(T) == 4) v = __fadd_rn(v, o.v);
+        else v = __hadd(v, o.v);
+    }
 };
 template <int VEC, typename T> __device__ __forceinline__ void store(T *p, const float (&v)[VEC])
 {
@@ -246,22 +280,15 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? 3 
 #pragma unroll
             for (int e = 0; e < VEC; ++e) u[i][e] = 0.f;
             if (has) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    u[i][e] = x[i].get(e);
-                    if constexpr (RES) u[i][e] = Elem<T>::get(Elem<T>::put(__fadd_rn(u[i][e], r[i].get(e))));
+                if constexpr (RES) {
+                    x[i].add(r[i]);
+                    if (a.h) x[i].put(static_cast<T *>(a.h) + row * a.ldh + (i * tpr + t) * VEC);
                 }
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) u[i][e] = x[i].get(e);
             }
         }
         ask(row + step);
-        if constexpr (RES) {
-            if (a.h && live) {
-                T *h = static_cast<T *>(a.h) + row * a.ldh;
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (i * tpr + t < n) store<VEC>(h + (i * tpr + t) * VEC, u[i]);
-            }
-        }
         int amax[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -292,44 +319,49 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? 3 
             for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
             if (tpr > 32 && lane == 0) warp_sum[odd][threadIdx.x >> 5] = sum;
         }
-        if (!direct || (NORM && tpr > 32)) __syncthreads();
-        float rstd = 1.f;
-        if constexpr (NORM) {
-            if (tpr > 32) {
-                const int warps = tpr >> 5;
-                sum = lane < warps ? warp_sum[odd][local * warps + lane] : 0.f;
-#pragma unroll
-                for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            }
-            rstd = rstd_of(sum, a);
-        }
-        if (!direct) {        // the other half is free: everybody is past last round's reads of it
+        if (!direct) {
+            __syncthreads();
+            // the other half is free: everybody is past last round's reads of it
             int *other = group_max + ((odd ^ 1) * per_cta + local) * a.G;
             for (int g = t; g < a.G; g += tpr) other[g] = 0;
         }
-        if (live) {
-            const int to = target_row(a, (int)row);
-            int8_t *codes = a.codes + (size_t)to * a.Cp;
+        const int to = live ? target_row(a, (int)row) : 0;
+        int8_t *codes = a.codes + (size_t)to * a.Cp;
+        float scale[NV];
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int v = i * tpr + t;
-                if (v < a.Cp / VEC) {
-                    float scale, inv;
-                    scale_of(__int_as_float(direct || v >= n ? amax[i] : gmax[group[i]]), scale, inv);
-                    if (to_scale[i]) to_scale[i][to] = NORM ? __fmul_rn(scale, rstd) : scale;
-                    uint32_t w[VEC];
+        for (int i = 0; i < NV; ++i) {
+            const int v = i * tpr + t;
+            float inv;
+            scale_of(__int_as_float(direct || v >= n ? amax[i] : gmax[group[i]]), scale[i], inv);
+            if (live && v < a.Cp / VEC) {
+                uint32_t w[VEC];
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) w[e] = code_bits(u[i][e], inv);
-                    if constexpr (VEC == 8) {
-                        uint32_t lo = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
-                        uint32_t hi = __byte_perm(__byte_perm(w[4], w[5], 0x0040), __byte_perm(w[6], w[7], 0x0040), 0x5410);
-                        if (!(inv > 0.f)) lo = hi = 0;
-                        *reinterpret_cast<uint2 *>(codes + v * 8) = make_uint2(lo, hi);
-                    } else {
-                        codes[v] = inv > 0.f ? (int8_t)w[0] : (int8_t)0;
-                    }
+                for (int e = 0; e < VEC; ++e) w[e] = code_bits(u[i][e], inv);
+                if constexpr (VEC == 8) {
+                    uint32_t lo = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
+                    uint32_t hi = __byte_perm(__byte_perm(w[4], w[5], 0x0040), __byte_perm(w[6], w[7], 0x0040), 0x5410);
+                    if (!(inv > 0.f)) lo = hi = 0;
+                    *reinterpret_cast<uint2 *>(codes + v * 8) = make_uint2(lo, hi);
+                } else {
+                    codes[v] = inv > 0.f ? (int8_t)w[0] : (int8_t)0;
                 }
             }
+        }
+        float rstd = 1.f;             // the scales alone wait for the row's sum
+        if constexpr (NORM) {
+            if (tpr > 32) {
+                if (direct) __syncthreads();
+                const float *part = warp_sum[odd] + local * (tpr >> 5);
+                sum = 0.f;
+#pragma unroll 4
+                for (int w = 0; w < tpr >> 5; ++w) sum += part[w];
+            }
+            rstd = rstd_of(sum, a);
+        }
+        if (live) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (to_scale[i]) to_scale[i][to] = NORM ? __fmul_rn(scale[i], rstd) : scale[i];
         }
         if (!direct) __syncthreads();     // the zeros are in place before the next round's maxima
     }
@@ -557,6 +589,7 @@ wfq_status_t wfq_rms_norm_quantize(const void *x_dev, long long ldx, const void 
     a.gs = a.G == 1 ? a.Cp : group_size;
     a.scale_pitch = (rows + 127LL) / 128 * 128;
     a.eps = eps;
+    a.per_C = 1.f / (float)C;
     return to_status(launch_rows(a, dtype, reinterpret_cast<cudaStream_t>(stream), true));
 }
 

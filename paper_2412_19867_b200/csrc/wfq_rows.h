@@ -23,7 +23,7 @@ struct RowsArgs {
     int gs = 0, G = 0;                // gs: a multiple of 32; one group: gs >= C
     long long scale_pitch = 0;
     int half = 0;                     // > 0: input row r goes to row 2 (r % half) + r / half (gated weights)
-    float eps = 0.f;
+    float eps = 0.f, per_C = 0.f;     // per_C: 1 / C
 };
 cudaError_t launch_rows(const RowsArgs &a, wfq_dtype_t dtype, cudaStream_t stream, bool pdl);
 
