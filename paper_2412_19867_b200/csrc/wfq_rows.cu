@@ -257,12 +257,16 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? 3 
     ask(row);
     // what a thread's vectors are to every row: their group, and whether they begin it
     int group[NV];
-    float *to_scale[NV];
+    float *to_scale[VEC == 1 ? 1 : NV];
+    if constexpr (VEC == 1) {                 // of step `lane`
+        const int c = lane * tpr + (t & ~31);
+        to_scale[0] = lane < NV && c < a.C && c % a.gs == 0 ? a.scales + (size_t)(c / a.gs) * a.scale_pitch : nullptr;
+    }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = (i * tpr + t) * VEC;
         group[i] = c / a.gs;
-        to_scale[i] = c < a.C && c == group[i] * a.gs ? a.scales + (size_t)group[i] * a.scale_pitch : nullptr;
+        if constexpr (VEC > 1) to_scale[i] = c < a.C && c == group[i] * a.gs ? a.scales + (size_t)group[i] * a.scale_pitch : nullptr;
         if constexpr (NORM) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) gain[i][e] = c < a.C ? __ldg(a.gain + c + e) : 0.f;
@@ -303,9 +307,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? 3 
             for (int e = 1; e < VEC; ++e) m = larger(m, u[i][e]);
             amax[i] = magnitude_bits(m);
         }
+        if constexpr (VEC == 1) {          // groups are multiples of 32: a warp's elements of a step are in one
+#pragma unroll
+            for (int i = 0; i < NV; ++i) amax[i] = __reduce_max_sync(0xffffffffu, amax[i]);
+        }
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1)
-            if (o < lanes) {
+            if (VEC > 1 && o < lanes) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i) amax[i] = max(amax[i], __shfl_xor_sync(0xffffffffu, amax[i], o));
             }
@@ -327,23 +335,37 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? 3 
         }
         const int to = live ? target_row(a, (int)row) : 0;
         int8_t *codes = a.codes + (size_t)to * a.Cp;
-        float scale[NV];
+        float scale[VEC == 1 ? 1 : NV];
+        if constexpr (VEC == 1) {
+            // one group per step and warp: lane i works out step i's scale for all
+            int m = 0;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int v = i * tpr + t;
+            for (int i = 0; i < NV; ++i) {
+                if (!direct && i * tpr + (t & ~31) < n) amax[i] = gmax[group[i]];      // the warp's, also of lanes behind the row
+                if (lane == i) m = amax[i];
+            }
             float inv;
-            scale_of(__int_as_float(direct || v >= n ? amax[i] : gmax[group[i]]), scale[i], inv);
-            if (live && v < a.Cp / VEC) {
-                uint32_t w[VEC];
+            scale_of(__int_as_float(m), scale[0], inv);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) w[e] = code_bits(u[i][e], inv);
-                if constexpr (VEC == 8) {
+            for (int i = 0; i < NV; ++i) {
+                const float iv = __shfl_sync(0xffffffffu, inv, i);
+                const int v = i * tpr + t;
+                if (live && v < a.Cp) codes[v] = iv > 0.f ? (int8_t)code_bits(u[i][0], iv) : (int8_t)0;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int v = i * tpr + t;
+                float inv;
+                scale_of(__int_as_float(direct || v >= n ? amax[i] : gmax[group[i]]), scale[i], inv);
+                if (live && v < a.Cp / VEC) {
+                    uint32_t w[VEC];
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) w[e] = code_bits(u[i][e], inv);
                     uint32_t lo = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
                     uint32_t hi = __byte_perm(__byte_perm(w[4], w[5], 0x0040), __byte_perm(w[6], w[7], 0x0040), 0x5410);
                     if (!(inv > 0.f)) lo = hi = 0;
                     *reinterpret_cast<uint2 *>(codes + v * 8) = make_uint2(lo, hi);
-                } else {
-                    codes[v] = inv > 0.f ? (int8_t)w[0] : (int8_t)0;
                 }
             }
         }
@@ -360,7 +382,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? 3 
         }
         if (live) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+            for (int i = 0; i < (VEC == 1 ? 1 : NV); ++i)
                 if (to_scale[i]) to_scale[i][to] = NORM ? __fmul_rn(scale[i], rstd) : scale[i];
         }
         if (!direct) __syncthreads();     // the zeros are in place before the next round's maxima
@@ -370,7 +392,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? 3 
 // Codes back to values, VEC of them at a time, four such pieces of a row on their way per thread.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) dequantize_kernel(const int8_t *__restrict__ codes, const float *__restrict__ scales,
-                                                         int rows, int C, int Cp, int gs, long long scale_pitch,
+                                                         int rows, int C, int Cp, FastDiv by_gs, long long scale_pitch,
                                                          T *__restrict__ v, long long ldv, int tpr)
 {
     constexpr int N = 4;
@@ -388,7 +410,7 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const int8_t *__restric
                 if (c < C) {
                     if constexpr (VEC == 8) q[i] = __ldg(reinterpret_cast<const uint2 *>(codes + row * Cp + c));
                     else q[i].x = (uint32_t)(uint8_t)__ldg(codes + row * Cp + c);
-                    s[i] = __ldg(scales + (size_t)(c / gs) * scale_pitch + row);
+                    s[i] = __ldg(scales + (size_t)(c / by_gs) * scale_pitch + row);
                 }
             }
 #pragma unroll
@@ -510,10 +532,10 @@ cudaError_t launch_dequantize(const int8_t *codes, const float *scales, int rows
     const int n = wide ? C / 8 : C, tpr = n >= 256 ? 256 : (n + 31) / 32 * 32, per_cta = 256 / tpr;
     const long long ctas = (rows + (long long)per_cta - 1) / per_cta, pitch = (rows + 127LL) / 128 * 128;
     const dim3 grid((unsigned)(ctas < (1 << 20) ? ctas : 1 << 20));
-    return wide ? launch(dequantize_kernel<T, 8>, grid, 256, 0, stream, true, codes, scales, rows, C, row_pitch_codes(C), gs,
-                         pitch, static_cast<T *>(v), ldv, tpr)
-                : launch(dequantize_kernel<T, 1>, grid, 256, 0, stream, true, codes, scales, rows, C, row_pitch_codes(C), gs,
-                         pitch, static_cast<T *>(v), ldv, tpr);
+    return wide ? launch(dequantize_kernel<T, 8>, grid, 256, 0, stream, true, codes, scales, rows, C, row_pitch_codes(C),
+                         FastDiv(gs), pitch, static_cast<T *>(v), ldv, tpr)
+                : launch(dequantize_kernel<T, 1>, grid, 256, 0, stream, true, codes, scales, rows, C, row_pitch_codes(C),
+                         FastDiv(gs), pitch, static_cast<T *>(v), ldv, tpr);
 }
 
 bool known(wfq_dtype_t t) { return t == WFQ_F32 || t == WFQ_F16 || t == WFQ_BF16; }
