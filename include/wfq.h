@@ -457,8 +457,8 @@ wfq_status_t wfq_linear_forward_codes(wfq_linear_t *lin, const int8_t *codes_dev
 /*
  * Test and profiling switches: WFQ_DEBUG_WAIT_CYCLES, WFQ_DEBUG_SKIP_GEMM_STAGE, and WFQ_DEBUG_GEMM_SHAPE (0: the
  * library chooses; else 10000 * CTAs that share a tile's channels (1, 2, 4, 8; at most one per 128 channels) + 1000 *
- * orientation (1: the accumulator's lanes are rows of x, 2: outputs, 3: rows of x over pairs of CTAs, not shared) +
- * columns per tile (1: 64, 128; 2: 16, 32, 64; 3: 128, 256)).
+ * orientation (1: the accumulator's lanes are rows of x, 2: outputs, 3: rows of x over pairs of CTAs, not shared; 4: dot
+ * products, taken for up to eight rows only) + columns per tile (1: 64, 128; 2: 16, 32, 64; 3: 128, 256; 4: 4)).
  */
 wfq_status_t wfq_linear_set_debug_option(wfq_linear_t *lin, wfq_debug_option_t option, long long value);
 

@@ -19,6 +19,7 @@
 #include <cuda_fp16.h>
 
 #include <new>
+#include <type_traits>
 
 #include "wfq_output_store.cuh"
 #include "wfq_ptx.cuh"
@@ -863,14 +864,222 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     }
 }
 
-// How a call is laid out: orientation (1: rows of x on the lanes, 2: outputs, 3: pairs of CTAs with rows of x), columns
-// per tile, CTAs that share a tile's channels.
+// Up to eight rows: linear_dot_kernel, dot products by the integer units (dp4a), bound by the weights' bytes.  A warp has
+// four columns of z and a part of the channels; a lane reads 16 channels of each column at a time, which lie in one group,
+// so their int32 sum is scaled at once and one fp32 sum per row and column is left to add over the lanes.  The rows' codes
+// are in shared memory; rows that come as values are quantized there by every CTA, which saves a launch.  The first
+// weights are asked for ahead of that, and ahead of the previous kernel's end where they are known to be in place.
+constexpr int DOT_THREADS = 256, DOT_WARPS = DOT_THREADS / 32, DOT_COLS = 4, DOT_AHEAD = 2;
+constexpr int DOT_MAX_ROWS = 8;
+constexpr int DOT_SMEM_MAX = 96 * 1024;
+
+struct DotArgs {
+    const void *x;               // values [rows][C], or null:
+    const int8_t *xq;            // codes and scales
+    const float *sx;
+    long long ldx, sx_pitch;
+    const int8_t *Wq;
+    const float *sW;
+    int C, Cp, G, rows, Kp;
+    int parts;                   // warps that share a column's channels: 1, 2, 4 or 8
+    int early;                   // the weights are complete whatever the previous kernel does
+    FastDiv by_gs, by_vectors;   // channels of a group; 8-channel vectors of a row
+    OutArgs out;
+};
+
+int dot_smem(int rows, int Cp, int G)
+{
+    const int r = rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8;
+    return r * Cp + 2 * 4 * r * G + DOT_WARPS * r * DOT_COLS * 4;
+}
+
+template <typename T> __device__ __forceinline__ float value_of(T v) { return (float)v; }
+
+template <int R, typename T>       // T: type of x, int8_t for codes
+__global__ void __launch_bounds__(DOT_THREADS) linear_dot_kernel(DotArgs a)
+{
+    extern __shared__ __align__(16) unsigned char smem_dot[];
+    int8_t *codes = reinterpret_cast<int8_t *>(smem_dot);                 // [R][Cp]
+    float *sx = reinterpret_cast<float *>(codes + R * a.Cp);              // [R][G]
+    int *gmax = reinterpret_cast<int *>(sx + R * a.G);                    // [R][G]
+    float *part = reinterpret_cast<float *>(gmax + R * a.G);              // [warp][R][DOT_COLS]
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int unit = (int)blockIdx.x * DOT_WARPS + warp, seg = unit % a.parts, k0 = unit / a.parts * DOT_COLS;
+    const int nv = a.Cp / 16, v0 = (int)((long long)nv * seg / a.parts), v1 = (int)((long long)nv * (seg + 1) / a.parts);
+    const int cols = min(DOT_COLS, a.out.Kz - k0);                        // none behind the last column
+    const uint4 *w = reinterpret_cast<const uint4 *>(a.Wq + (size_t)k0 * a.Cp);
+
+    uint4 now[DOT_AHEAD][DOT_COLS], next[DOT_AHEAD][DOT_COLS];
+    auto fetch = [&](uint4 (&to)[DOT_AHEAD][DOT_COLS], int v) {
+#pragma unroll
+        for (int u = 0; u < DOT_AHEAD; ++u)
+#pragma unroll
+            for (int j = 0; j < DOT_COLS; ++j)
+                if (j < cols && v + 32 * u < v1) to[u][j] = __ldg(w + (size_t)j * nv + v + 32 * u);
+    };
+    if (!a.early) ptx::grid_dependency_wait();
+    fetch(now, v0 + lane);
+    if (a.early) ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
+
+    // ---- the rows' codes and scales ----
+    if constexpr (std::is_same<T, int8_t>::value) {
+        const int n = a.Cp / 16;
+        for (int i = threadIdx.x; i < R * n; i += DOT_THREADS)
+            reinterpret_cast<uint4 *>(codes)[i] =
+                i < a.rows * n ? reinterpret_cast<const uint4 *>(a.xq)[i] : make_uint4(0, 0, 0, 0);
+        for (int i = threadIdx.x; i < R * a.G; i += DOT_THREADS) {
+            const int r = i / a.G, g = i - r * a.G;
+            sx[i] = r < a.rows ? a.sx[(size_t)g * a.sx_pitch + r] : 0.f;
+        }
+    } else {
+        for (int i = threadIdx.x; i < R * a.G; i += DOT_THREADS) gmax[i] = 0;
+        __syncthreads();
+        const int vec = a.Cp / 8, total = a.rows * vec;                   // vectors of eight channels, four to 32
+        const bool wide = a.C % 8 == 0 && a.ldx * sizeof(T) % 16 == 0 && (reinterpret_cast<uintptr_t>(a.x) & 15) == 0;
+        constexpr int KEEP = 4;
+        float u[KEEP][8];
+        auto load = [&](int i, float (&to)[8]) {
+            const int r = i / a.by_vectors, c = (i - r * vec) * 8;
+            const T *p = static_cast<const T *>(a.x) + r * a.ldx + c;
+            if (wide) {
+                if (c >= a.C) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) to[e] = 0.f;
+                } else if constexpr (sizeof(T) == 4) {
+                    const float4 lo = reinterpret_cast<const float4 *>(p)[0], hi = reinterpret_cast<const float4 *>(p)[1];
+                    to[0] = lo.x; to[1] = lo.y; to[2] = lo.z; to[3] = lo.w;
+                    to[4] = hi.x; to[5] = hi.y; to[6] = hi.z; to[7] = hi.w;
+                } else {
+                    const uint4 q = *reinterpret_cast<const uint4 *>(p);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) to[e] = value_of(reinterpret_cast<const T *>(&q)[e]);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) to[e] = c + e < a.C ? value_of(p[e]) : 0.f;
+            }
+        };
+        auto group_at = [&](int i) {          // index of the group of vector i, row by row
+            const int r = i / a.by_vectors;
+            return r * a.G + (i - r * vec) * 8 / a.by_gs;
+        };
+        // vectors beyond what registers keep are read again for their codes
+        const int rounds = (total + DOT_THREADS - 1) / DOT_THREADS;
+        for (int pass = 0; pass < 2; ++pass) {
+            for (int k0r = 0; k0r < rounds; k0r += KEEP) {
+                if (pass == 0 || rounds > KEEP) {
+#pragma unroll
+                    for (int k = 0; k < KEEP; ++k) {
+                        const int i = (k0r + k) * DOT_THREADS + threadIdx.x;
+                        if (i < total) load(i, u[k]);
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < KEEP; ++k) {
+                    const int i = (k0r + k) * DOT_THREADS + threadIdx.x;
+                    if (pass == 0) {
+                        int m = 0;
+                        if (i < total) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) m = max(m, __float_as_int(u[k][e]) & 0x7fffffff);
+                        }
+                        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                        m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                        if (i < total && (lane & 3) == 0) atomicMax(&gmax[group_at(i)], m);
+                    } else if (i < total) {
+                        float scale, inv;
+                        quantizer_scale(__int_as_float(gmax[group_at(i)]), scale, inv);
+                        uint32_t q[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) q[e] = inv > 0.f ? code_bits(u[k][e], inv) : 0u;
+                        const uint32_t lo = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+                        const uint32_t hi = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+                        reinterpret_cast<uint2 *>(codes)[i] = make_uint2(lo, hi);
+                    }
+                }
+            }
+            if (pass == 0) {
+                __syncthreads();
+                for (int i = threadIdx.x; i < a.rows * a.G; i += DOT_THREADS) {
+                    float inv;
+                    quantizer_scale(__int_as_float(gmax[i]), sx[i], inv);
+                }
+            }
+        }
+        for (int i = total + threadIdx.x; i < R * vec; i += DOT_THREADS) reinterpret_cast<uint2 *>(codes)[i] = make_uint2(0, 0);
+        for (int i = a.rows * a.G + threadIdx.x; i < R * a.G; i += DOT_THREADS) sx[i] = 0.f;
+    }
+    __syncthreads();
+
+    // ---- dot products ----
+    float acc[R][DOT_COLS];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int j = 0; j < DOT_COLS; ++j) acc[r][j] = 0.f;
+    for (int v = v0 + lane; v < v1 + lane; v += 32 * DOT_AHEAD) {        // the same number of turns for all lanes
+        fetch(next, v + 32 * DOT_AHEAD);
+#pragma unroll
+        for (int u = 0; u < DOT_AHEAD; ++u) {
+            const int vu = v + 32 * u;
+            if (vu < v1 && cols > 0) {
+                const int g = vu * 16 / a.by_gs;
+                const float4 sw = __ldg(reinterpret_cast<const float4 *>(a.sW + (size_t)g * a.Kp + k0));
+                const float s[DOT_COLS] = {sw.x, sw.y, sw.z, sw.w};
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const uint4 q = *reinterpret_cast<const uint4 *>(codes + r * a.Cp + vu * 16);
+                    const float sr = sx[r * a.G + g];
+#pragma unroll
+                    for (int j = 0; j < DOT_COLS; ++j) {
+                        int d = __dp4a((int)q.x, (int)now[u][j].x, 0);
+                        d = __dp4a((int)q.y, (int)now[u][j].y, d);
+                        d = __dp4a((int)q.z, (int)now[u][j].z, d);
+                        d = __dp4a((int)q.w, (int)now[u][j].w, d);
+                        acc[r][j] = fmaf((float)d * sr, s[j], acc[r][j]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < DOT_COLS; ++j) now[u][j] = next[u][j];
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int j = 0; j < DOT_COLS; ++j)
+#pragma unroll
+            for (int o = 16; o; o >>= 1) acc[r][j] += __shfl_xor_sync(0xffffffffu, acc[r][j], o);
+    // lane 2 r + p finishes columns 2 p and 2 p + 1 of row r
+    float f0 = 0.f, f1 = 0.f;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int p = 0; p < DOT_COLS / 2; ++p)
+            if (lane == 2 * r + p) { f0 = acc[r][2 * p]; f1 = acc[r][2 * p + 1]; }
+    if (a.parts > 1) {
+        float *mine = part + warp * R * DOT_COLS;
+        if (lane < 2 * R) { mine[2 * lane] = f0; mine[2 * lane + 1] = f1; }
+        __syncthreads();
+        if (seg == 0 && lane < 2 * R)
+            for (int p = 1; p < a.parts; ++p) {       // in order
+                f0 += part[(warp + p) * R * DOT_COLS + 2 * lane];
+                f1 += part[(warp + p) * R * DOT_COLS + 2 * lane + 1];
+            }
+    }
+    if (seg == 0 && lane < 2 * R) finish_pair(a.out, lane / 2, k0 + 2 * (lane & 1), f0, f1);
+}
+
+// How a call is laid out: orientation (1: rows of x on the lanes, 2: outputs, 3: pairs of CTAs with rows of x, 4: dot
+// products), columns per tile, CTAs that share a tile's channels.
 struct Shape { int orient, bn, split; };
 
 bool known_shape(const Shape &s)
 {
     if (s.orient == 1) return s.bn == 64 || s.bn == 128;
     if (s.orient == 2) return s.bn == 16 || s.bn == 32 || s.bn == 64;
+    if (s.orient == 4) return s.bn == 4 && s.split == 1;
     return s.orient == 3 && s.split == 1 && (s.bn == 128 || s.bn == 256);
 }
 
@@ -885,7 +1094,10 @@ TileTime tile_time(const Shape &s)
 
 Shape choose(const wfq_linear &l, int rows)
 {
-    if (l.debug_shape) return Shape{l.debug_shape / 1000 % 10, l.debug_shape % 1000, l.debug_shape / 10000};
+    const bool dot = rows <= DOT_MAX_ROWS && dot_smem(rows, l.Cp, l.G) <= DOT_SMEM_MAX;
+    if (l.debug_shape && (dot || l.debug_shape / 1000 % 10 != 4))
+        return Shape{l.debug_shape / 1000 % 10, l.debug_shape % 1000, l.debug_shape / 10000};
+    if (dot) return Shape{4, 4, 1};
     const int KB = (l.Cp / 32 + 3) / 4;
     Shape best{1, 64, 1};
     double best_cost = 1e300;
@@ -958,14 +1170,80 @@ cudaError_t launch_variant(const wfq_linear &l, MmaArgs &a, int grid, const int8
     return cudaLaunchKernelEx(&cfg, linear_mma_kernel<BN, SWAP, PAIR>, SWAP ? tw : tx, SWAP ? tx : tw, a);
 }
 
-cudaError_t launch_product(wfq_linear &l, const int8_t *xq, const float *sx, int rows, const OutArgs &out,
-                           cudaStream_t stream, bool pdl)
+template <int R, typename T>
+cudaError_t launch_dot_kernel(const DotArgs &a, int grid, int smem, cudaStream_t stream, bool pdl)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(DOT_THREADS);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, linear_dot_kernel<R, T>, a);
+}
+template <typename T>
+cudaError_t launch_dot_rows(const DotArgs &a, int grid, int smem, cudaStream_t stream, bool pdl)
+{
+    if (a.rows <= 1) return launch_dot_kernel<1, T>(a, grid, smem, stream, pdl);
+    if (a.rows <= 2) return launch_dot_kernel<2, T>(a, grid, smem, stream, pdl);
+    if (a.rows <= 4) return launch_dot_kernel<4, T>(a, grid, smem, stream, pdl);
+    return launch_dot_kernel<8, T>(a, grid, smem, stream, pdl);
+}
+template <typename T>
+cudaError_t setup_dot()
+{
+    cudaError_t e = cudaSuccess;
+    auto set = [&](auto kernel) {
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, DOT_SMEM_MAX);
+    };
+    set(linear_dot_kernel<1, T>);
+    set(linear_dot_kernel<2, T>);
+    set(linear_dot_kernel<4, T>);
+    set(linear_dot_kernel<8, T>);
+    return e;
+}
+
+// x: values in the layer's input type, or null with codes and scales.
+cudaError_t launch_dot(const wfq_linear &l, const void *x, long long ldx, const int8_t *xq, const float *sx, int rows,
+                       const OutArgs &out, cudaStream_t stream, bool pdl)
+{
+    DotArgs a;
+    a.x = x; a.ldx = ldx;
+    a.xq = xq; a.sx = sx; a.sx_pitch = (rows + 127LL) / 128 * 128;
+    a.Wq = l.Wq; a.sW = l.sW;
+    a.C = l.C; a.Cp = l.Cp; a.G = l.G; a.rows = rows; a.Kp = l.Kp;
+    a.by_gs = FastDiv(l.gs);
+    a.by_vectors = FastDiv(l.Cp / 8);
+    a.early = pdl;
+    a.out = out;
+    // as many warps to a column as give every SM two CTAs, but a lane two vectors at least
+    const int quads = (l.Kz + DOT_COLS - 1) / DOT_COLS;
+    a.parts = 1;
+    while (a.parts < 8 && (long long)quads * a.parts < 16LL * l.sm_count && l.Cp / 16 / (2 * a.parts) >= 64) a.parts *= 2;
+    const int grid = (int)(((long long)quads * a.parts + DOT_WARPS - 1) / DOT_WARPS), smem = dot_smem(rows, l.Cp, l.G);
+    if (!x) return launch_dot_rows<int8_t>(a, grid, smem, stream, pdl);
+    if (l.in_dtype == WFQ_F32) return launch_dot_rows<float>(a, grid, smem, stream, pdl);
+    if (l.in_dtype == WFQ_F16) return launch_dot_rows<__half>(a, grid, smem, stream, pdl);
+    return launch_dot_rows<__nv_bfloat16>(a, grid, smem, stream, pdl);
+}
+
+const Shape shape_for(wfq_linear &l, int rows)
 {
     if (l.shape_rows != rows) {
         const Shape s = choose(l, rows);
         l.shape_rows = rows; l.shape_orient = s.orient; l.shape_bn = s.bn; l.shape_split = s.split;
     }
-    const Shape sp{l.shape_orient, l.shape_bn, l.shape_split};
+    return Shape{l.shape_orient, l.shape_bn, l.shape_split};
+}
+
+cudaError_t launch_product(wfq_linear &l, const int8_t *xq, const float *sx, int rows, const OutArgs &out,
+                           cudaStream_t stream, bool pdl)
+{
+    const Shape sp = shape_for(l, rows);
     MmaArgs a;
     const long long sx_pitch = (rows + 127LL) / 128 * 128;
     const bool swap = sp.orient == 2, pair = sp.orient == 3;
@@ -1024,6 +1302,10 @@ wfq_status_t bind(wfq_linear *l)
     if (e == cudaSuccess) e = setup_variant<128, false, false>();
     if (e == cudaSuccess) e = setup_variant<128, false, true>();
     if (e == cudaSuccess) e = setup_variant<256, false, true>();
+    if (e == cudaSuccess) e = setup_dot<int8_t>();
+    if (e == cudaSuccess) e = setup_dot<float>();
+    if (e == cudaSuccess) e = setup_dot<__half>();
+    if (e == cudaSuccess) e = setup_dot<__nv_bfloat16>();
     if (e != cudaSuccess) return WFQ_ERR_CUDA;
     l->device = dev;
     l->sm_count = sms;
@@ -1040,18 +1322,10 @@ wfq_status_t check_io(const wfq_linear *l, int rows, const void *residual, long 
     return WFQ_OK;
 }
 
-wfq_status_t product(wfq_linear *l, const int8_t *xq, const float *sx, int rows, const void *residual, long long ldr,
-                     void *y, long long ldy, cudaStream_t st, bool weights_waited_for)
+// The layer on codes, or on values `x` (then xq and sx are the workspace).
+wfq_status_t run(wfq_linear *l, const void *x, long long ldx, int8_t *xq, float *sx, int rows, const void *residual,
+                 long long ldr, void *y, long long ldy, cudaStream_t st)
 {
-    // The launch may begin before the previous kernel has ended.  Weights that were written since are waited for by an
-    // ordinary launch; not forgotten under capture, where the launch is only recorded.
-    bool pdl = true;
-    if (l->fresh && !weights_waited_for) {
-        pdl = false;
-        cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
-        if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) return WFQ_ERR_CUDA;
-        if (cap == cudaStreamCaptureStatusNone) l->fresh = false;
-    }
     OutArgs o;
     o.bias = l->bias; o.residual = residual; o.y = y;
     o.ldr = ldr; o.ldy = ldy;
@@ -1059,6 +1333,30 @@ wfq_status_t product(wfq_linear *l, const int8_t *xq, const float *sx, int rows,
     o.act = l->act; o.gated = l->gated; o.dtype = (int)l->out_dtype;
     const size_t e = elem_bytes(l->out_dtype);
     o.vec = !misaligned(y, 16) && ldy * e % 16 == 0 && (!residual || (!misaligned(residual, 16) && ldr * e % 16 == 0));
+
+    const bool dot = shape_for(*l, rows).orient == 4;
+    const bool quantize = x && !dot;
+    if (quantize) {
+        RowsArgs a;
+        a.x = x; a.ldx = ldx;
+        a.codes = xq; a.scales = sx;
+        a.rows = rows; a.C = l->C; a.Cp = l->Cp;
+        a.gs = l->gs; a.G = l->G;
+        a.scale_pitch = (rows + 127LL) / 128 * 128;
+        if (launch_rows(a, l->in_dtype, st, true) != cudaSuccess) return WFQ_ERR_CUDA;
+    }
+    // The product's launch may begin before the kernel in front of it has ended, and fetches weights then.  The row
+    // quantizer lets it begin only after its own wait for what was in front of it, fresh weights too; without it, weights
+    // that were written since are waited for by an ordinary launch.  Under capture the launch is only recorded, and the
+    // weights stay fresh.
+    bool pdl = true;
+    if (l->fresh && !quantize) {
+        pdl = false;
+        cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+        if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) return WFQ_ERR_CUDA;
+        if (cap == cudaStreamCaptureStatusNone) l->fresh = false;
+    }
+    if (dot) return to_status(launch_dot(*l, x, ldx, xq, sx, rows, o, st, pdl));
     return to_status(launch_product(*l, xq, sx, rows, o, st, pdl));
 }
 
@@ -1174,8 +1472,8 @@ wfq_status_t wfq_linear_forward_codes(wfq_linear_t *l, const int8_t *codes_dev, 
     if (s != WFQ_OK) return s;
     if (!codes_dev || !scales_dev || misaligned(codes_dev, 32) || misaligned(scales_dev, 16)) return WFQ_ERR_INVALID_ARG;
     if ((s = bind(l)) != WFQ_OK) return s;
-    return product(l, codes_dev, scales_dev, rows, residual_dev, ldr, y_dev, ldy, reinterpret_cast<cudaStream_t>(stream),
-                   false);
+    return run(l, nullptr, 0, const_cast<int8_t *>(codes_dev), const_cast<float *>(scales_dev), rows, residual_dev, ldr,
+               y_dev, ldy, reinterpret_cast<cudaStream_t>(stream));
 }
 
 wfq_status_t wfq_linear_forward(wfq_linear_t *l, const void *x_dev, long long ldx, int rows, const void *residual_dev,
@@ -1189,16 +1487,7 @@ wfq_status_t wfq_linear_forward(wfq_linear_t *l, const void *x_dev, long long ld
     if (!x_dev || ldx < l->C || misaligned(x_dev, elem_bytes(l->in_dtype)) || rows > l->max_rows)
         return WFQ_ERR_INVALID_ARG;
     if ((s = bind(l)) != WFQ_OK) return s;
-    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    RowsArgs a;
-    a.x = x_dev; a.ldx = ldx;
-    a.codes = l->xq; a.scales = l->sx;
-    a.rows = rows; a.C = l->C; a.Cp = l->Cp;
-    a.gs = l->gs; a.G = l->G;
-    a.scale_pitch = (rows + 127LL) / 128 * 128;
-    if (launch_rows(a, l->in_dtype, st, true) != cudaSuccess) return WFQ_ERR_CUDA;
-    // the row quantizer lets the product start only after its own wait for what was in front of it, fresh weights too
-    return product(l, l->xq, l->sx, rows, residual_dev, ldr, y_dev, ldy, st, true);
+    return run(l, x_dev, ldx, l->xq, l->sx, rows, residual_dev, ldr, y_dev, ldy, reinterpret_cast<cudaStream_t>(stream));
 }
 
 wfq_status_t wfq_linear_set_debug_option(wfq_linear_t *l, wfq_debug_option_t option, long long value)

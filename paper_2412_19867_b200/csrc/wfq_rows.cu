@@ -19,8 +19,6 @@ namespace wfq {
 
 namespace {
 
-constexpr int kNonFinite = 0x7f800000;    // bit patterns of |v| from here on are infinities and NaN
-
 template <typename T> struct Elem;
 template <> struct Elem<float> {
     static __device__ __forceinline__ float get(float v) { return v; }
@@ -50,28 +48,6 @@ template <typename T> __device__ __forceinline__ void store8(T *p, const float (
     }
 }
 
-// Scale amax / 127 and reciprocal 127 / amax of a group, both correctly rounded: a quotient from an approximate reciprocal
-// is corrected by its remainder (Markstein's method), which gives the bits of __fdiv_rn for every float from 1e-30 to the
-// largest in a fraction of the instructions.  A group that holds an infinity or a NaN has the scale NaN and codes 0, so that
-// what is computed from it is NaN; inv is 0 where the codes are.
-__device__ __forceinline__ void scale_of(float amax, float &scale, float &inv)
-{
-    constexpr float r127 = 1.f / 127.f;
-    float q = __fmul_rn(amax, r127);
-    scale = fmaf(fmaf(-127.f, q, amax), r127, q);
-    float r;
-    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(amax));
-    r = fmaf(r, fmaf(-amax, r, 1.f), r);
-    q = __fmul_rn(127.f, r);
-    inv = fmaf(fmaf(-amax, q, 127.f), r, q);
-    if (!(amax >= 1e-30f)) scale = inv = 0.f;
-    if (!(amax < __int_as_float(kNonFinite))) { scale = __int_as_float(0x7fc00000); inv = 0.f; }
-}
-__device__ __forceinline__ uint32_t code_bits(float u, float inv)
-{
-    // product and sum rounded separately, as the quantizer is defined; the low byte of the sum is the code
-    return __float_as_uint(__fadd_rn(__fmul_rn(u, inv), 12582912.f));
-}
 // The larger magnitude; NaN where one of the two is.
 __device__ __forceinline__ float larger(float m, float u)
 {
@@ -141,13 +117,13 @@ __global__ void __launch_bounds__(256) rows_any_kernel(RowsArgs a)
         const int to = target_row(a, row);
         for (int g = threadIdx.x; g < a.G; g += 256) {
             float scale, inv;
-            scale_of(__int_as_float(group_max[g]), scale, inv);
+            quantizer_scale(__int_as_float(group_max[g]), scale, inv);
             a.scales[(size_t)g * a.scale_pitch + to] = NORM ? __fmul_rn(scale, rstd) : scale;
         }
         for (int c0 = warp * 32; c0 < a.Cp; c0 += 256) {
             const int c = c0 + lane;
             float scale, inv;
-            scale_of(__int_as_float(group_max[c0 / a.gs]), scale, inv);
+            quantizer_scale(__int_as_float(group_max[c0 / a.gs]), scale, inv);
             uint32_t code = 0;
             if (c < a.C && inv > 0.f) {
                 float u = value(c, true);
@@ -345,7 +321,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? 3 
                 if (lane == i) m = amax[i];
             }
             float inv;
-            scale_of(__int_as_float(m), scale[0], inv);
+            quantizer_scale(__int_as_float(m), scale[0], inv);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const float iv = __shfl_sync(0xffffffffu, inv, i);
@@ -357,7 +333,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? 3 
             for (int i = 0; i < NV; ++i) {
                 const int v = i * tpr + t;
                 float inv;
-                scale_of(__int_as_float(direct || v >= n ? amax[i] : gmax[group[i]]), scale[i], inv);
+                quantizer_scale(__int_as_float(direct || v >= n ? amax[i] : gmax[group[i]]), scale[i], inv);
                 if (live && v < a.Cp / VEC) {
                     uint32_t w[VEC];
 #pragma unroll

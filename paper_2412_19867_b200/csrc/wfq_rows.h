@@ -30,4 +30,29 @@ cudaError_t launch_rows(const RowsArgs &a, wfq_dtype_t dtype, cudaStream_t strea
 // Compute capability and SM count of the current device, looked up once per device.
 wfq_status_t current_device(int *device, int *sm_count);
 
+#ifdef __CUDACC__
+// Scale amax / 127 and reciprocal 127 / amax of a group, both correctly rounded: a quotient from an approximate reciprocal
+// is corrected by its remainder (Markstein's method), which gives the bits of __fdiv_rn for every float from 1e-30 to the
+// largest in a fraction of the instructions.  A group that holds an infinity or a NaN has the scale NaN and codes 0, so that
+// what is computed from it is NaN; inv is 0 where the codes are.
+__device__ __forceinline__ void quantizer_scale(float amax, float &scale, float &inv)
+{
+    constexpr float r127 = 1.f / 127.f;
+    float q = __fmul_rn(amax, r127);
+    scale = fmaf(fmaf(-127.f, q, amax), r127, q);
+    float r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(amax));
+    r = fmaf(r, fmaf(-amax, r, 1.f), r);
+    q = __fmul_rn(127.f, r);
+    inv = fmaf(fmaf(-amax, q, 127.f), r, q);
+    if (!(amax >= 1e-30f)) scale = inv = 0.f;
+    if (!(amax < __int_as_float(0x7f800000))) { scale = __int_as_float(0x7fc00000); inv = 0.f; }
+}
+__device__ __forceinline__ uint32_t code_bits(float u, float inv)
+{
+    // product and sum rounded separately, as the quantizer is defined; the low byte of the sum is the code
+    return __float_as_uint(__fadd_rn(__fmul_rn(u, inv), 12582912.f));
+}
+#endif
+
 }  // namespace wfq

@@ -111,7 +111,7 @@ def test_settings(lib):
     assert lib.wfq_linear_set_epilogue(lin, ctypes.c_void_p(4097), 0) == INVALID
     ll = ctypes.c_longlong
     for value, want in ((0, OK), (11064, OK), (41128, OK), (42016, OK), (13256, OK), (23256, INVALID), (11256, INVALID), (82016, INVALID), (31064, INVALID), (11032, INVALID),
-                        (12128, INVALID), (13064, INVALID), (14064, INVALID), (111064, INVALID), (1064, INVALID), (-11064, INVALID)):
+                        (12128, INVALID), (13064, INVALID), (14064, INVALID), (14004, OK), (24004, INVALID), (111064, INVALID), (1064, INVALID), (-11064, INVALID)):
         assert lib.wfq_linear_set_debug_option(lin, b.WFQ_DEBUG_GEMM_SHAPE, ll(value)) == want, value
     assert lib.wfq_linear_set_debug_option(lin, b.WFQ_DEBUG_WAIT_CYCLES, ll(999)) == INVALID
     assert lib.wfq_linear_set_debug_option(lin, b.WFQ_DEBUG_SKIP_GEMM_STAGE, ll(-2)) == INVALID
