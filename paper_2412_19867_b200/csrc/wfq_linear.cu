@@ -483,6 +483,16 @@ __device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, cons
     const bool active = row0 + quarter * 32 < a.rows && col0 + ec.c0 < a.cols;
     Sums<CW, SWAP> sums;
     sums.zero();
+    if constexpr (!SWAP) {
+        // the residual's lines on their way to L2 while the sums are formed (4096 x 128 -> 4096 fp32 66 -> 50 us; asking for
+        // them in registers ahead of their use costs the promotion more in spills than it gains here)
+        const long long r = row0 + quarter * 32 + lane;
+        if (a.out.residual && active && a.split == 1 && r < a.out.R) {
+            const int elem = a.out.dtype == WFQ_F32 ? 4 : 2, j0 = (col0 + ec.c0) >> a.out.gated, n = CW >> a.out.gated;
+            const char *line = static_cast<const char *>(a.out.residual) + (r * a.out.ldr + j0) * elem;
+            for (int i = 0; i < n && j0 + i < a.out.K; i += 128 / elem) ptx::prefetch_l2(line + i * elem);
+        }
+    }
     bool ready = false;              // the slot was seen to be full ahead of its turn
     for (int q0 = 0; q0 < rg.np; q0 += a.cg) {
         const int n = min(a.cg, rg.np - q0);
@@ -872,6 +882,10 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
 constexpr int DOT_THREADS = 256, DOT_WARPS = DOT_THREADS / 32, DOT_COLS = 4, DOT_AHEAD = 2;
 constexpr int DOT_MAX_ROWS = 8;
 constexpr int DOT_SMEM_MAX = 96 * 1024;
+// Values that a CTA quantizes for itself: as many as its registers keep.  Beyond, reading them twice in every CTA takes
+// longer than a launch (4 rows of 8192 channels: 46 us).
+constexpr int DOT_KEEP = 4;
+constexpr int DOT_QUANTIZE_MAX = 8 * DOT_THREADS * DOT_KEEP;
 
 struct DotArgs {
     const void *x;               // values [rows][C], or null:
@@ -882,6 +896,7 @@ struct DotArgs {
     const float *sW;
     int C, Cp, G, rows, Kp;
     int parts;                   // warps that share a column's channels: 1, 2, 4 or 8
+    int units;                   // blocks of DOT_COLS columns times parts
     int early;                   // the weights are complete whatever the previous kernel does
     FastDiv by_gs, by_vectors;   // channels of a group; 8-channel vectors of a row
     OutArgs out;
@@ -904,21 +919,25 @@ __global__ void __launch_bounds__(DOT_THREADS) linear_dot_kernel(DotArgs a)
     int *gmax = reinterpret_cast<int *>(sx + R * a.G);                    // [R][G]
     float *part = reinterpret_cast<float *>(gmax + R * a.G);              // [warp][R][DOT_COLS]
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int unit = (int)blockIdx.x * DOT_WARPS + warp, seg = unit % a.parts, k0 = unit / a.parts * DOT_COLS;
+    // One unit per warp where warps share a column; else a warp goes on to further units, their weights in one stream
+    int unit = (int)blockIdx.x * DOT_WARPS + warp;
+    const int seg = unit % a.parts, units = a.units, stride = a.parts > 1 ? units : (int)gridDim.x * DOT_WARPS;
     const int nv = a.Cp / 16, v0 = (int)((long long)nv * seg / a.parts), v1 = (int)((long long)nv * (seg + 1) / a.parts);
-    const int cols = min(DOT_COLS, a.out.Kz - k0);                        // none behind the last column
-    const uint4 *w = reinterpret_cast<const uint4 *>(a.Wq + (size_t)k0 * a.Cp);
 
     uint4 now[DOT_AHEAD][DOT_COLS], next[DOT_AHEAD][DOT_COLS];
-    auto fetch = [&](uint4 (&to)[DOT_AHEAD][DOT_COLS], int v) {
+    auto fetch = [&](uint4 (&to)[DOT_AHEAD][DOT_COLS], int of, int v) {
+        if (of >= units) return;
+        const int k = of / a.parts * DOT_COLS;
+        const uint4 *w = reinterpret_cast<const uint4 *>(a.Wq + (size_t)k * a.Cp) + v;
+        const int cols = a.out.Kz - k;
 #pragma unroll
         for (int u = 0; u < DOT_AHEAD; ++u)
 #pragma unroll
             for (int j = 0; j < DOT_COLS; ++j)
-                if (j < cols && v + 32 * u < v1) to[u][j] = __ldg(w + (size_t)j * nv + v + 32 * u);
+                if (j < cols && v + 32 * u < v1) to[u][j] = __ldg(w + (size_t)j * nv + 32 * u);
     };
     if (!a.early) ptx::grid_dependency_wait();
-    fetch(now, v0 + lane);
+    fetch(now, unit, v0 + lane);
     if (a.early) ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
 
@@ -937,8 +956,7 @@ __global__ void __launch_bounds__(DOT_THREADS) linear_dot_kernel(DotArgs a)
         __syncthreads();
         const int vec = a.Cp / 8, total = a.rows * vec;                   // vectors of eight channels, four to 32
         const bool wide = a.C % 8 == 0 && a.ldx * sizeof(T) % 16 == 0 && (reinterpret_cast<uintptr_t>(a.x) & 15) == 0;
-        constexpr int KEEP = 4;
-        float u[KEEP][8];
+        float u[DOT_KEEP][8];
         auto load = [&](int i, float (&to)[8]) {
             const int r = i / a.by_vectors, c = (i - r * vec) * 8;
             const T *p = static_cast<const T *>(a.x) + r * a.ldx + c;
@@ -964,47 +982,40 @@ __global__ void __launch_bounds__(DOT_THREADS) linear_dot_kernel(DotArgs a)
             const int r = i / a.by_vectors;
             return r * a.G + (i - r * vec) * 8 / a.by_gs;
         };
-        // vectors beyond what registers keep are read again for their codes
-        const int rounds = (total + DOT_THREADS - 1) / DOT_THREADS;
-        for (int pass = 0; pass < 2; ++pass) {
-            for (int k0r = 0; k0r < rounds; k0r += KEEP) {
-                if (pass == 0 || rounds > KEEP) {
 #pragma unroll
-                    for (int k = 0; k < KEEP; ++k) {
-                        const int i = (k0r + k) * DOT_THREADS + threadIdx.x;
-                        if (i < total) load(i, u[k]);
-                    }
-                }
+        for (int k = 0; k < DOT_KEEP; ++k) {
+            const int i = k * DOT_THREADS + threadIdx.x;
+            if (i < total) load(i, u[k]);
+        }
 #pragma unroll
-                for (int k = 0; k < KEEP; ++k) {
-                    const int i = (k0r + k) * DOT_THREADS + threadIdx.x;
-                    if (pass == 0) {
-                        int m = 0;
-                        if (i < total) {
+        for (int k = 0; k < DOT_KEEP; ++k) {
+            const int i = k * DOT_THREADS + threadIdx.x;
+            int m = 0;
+            if (i < total) {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) m = max(m, __float_as_int(u[k][e]) & 0x7fffffff);
-                        }
-                        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-                        m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-                        if (i < total && (lane & 3) == 0) atomicMax(&gmax[group_at(i)], m);
-                    } else if (i < total) {
-                        float scale, inv;
-                        quantizer_scale(__int_as_float(gmax[group_at(i)]), scale, inv);
-                        uint32_t q[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) q[e] = inv > 0.f ? code_bits(u[k][e], inv) : 0u;
-                        const uint32_t lo = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
-                        const uint32_t hi = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
-                        reinterpret_cast<uint2 *>(codes)[i] = make_uint2(lo, hi);
-                    }
-                }
+                for (int e = 0; e < 8; ++e) m = max(m, __float_as_int(u[k][e]) & 0x7fffffff);
             }
-            if (pass == 0) {
-                __syncthreads();
-                for (int i = threadIdx.x; i < a.rows * a.G; i += DOT_THREADS) {
-                    float inv;
-                    quantizer_scale(__int_as_float(gmax[i]), sx[i], inv);
-                }
+            m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));      // the four lanes of 32 channels
+            m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+            if (i < total && (lane & 3) == 0) atomicMax(&gmax[group_at(i)], m);
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.rows * a.G; i += DOT_THREADS) {
+            float inv;
+            quantizer_scale(__int_as_float(gmax[i]), sx[i], inv);
+        }
+#pragma unroll
+        for (int k = 0; k < DOT_KEEP; ++k) {
+            const int i = k * DOT_THREADS + threadIdx.x;
+            if (i < total) {
+                float scale, inv;
+                quantizer_scale(__int_as_float(gmax[group_at(i)]), scale, inv);
+                uint32_t q[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) q[e] = inv > 0.f ? code_bits(u[k][e], inv) : 0u;
+                const uint32_t lo = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+                const uint32_t hi = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+                reinterpret_cast<uint2 *>(codes)[i] = make_uint2(lo, hi);
             }
         }
         for (int i = total + threadIdx.x; i < R * vec; i += DOT_THREADS) reinterpret_cast<uint2 *>(codes)[i] = make_uint2(0, 0);
@@ -1013,62 +1024,74 @@ __global__ void __launch_bounds__(DOT_THREADS) linear_dot_kernel(DotArgs a)
     __syncthreads();
 
     // ---- dot products ----
-    float acc[R][DOT_COLS];
+    for (; unit < units; unit += stride) {
+        const int k0 = unit / a.parts * DOT_COLS;
+        float acc[R][DOT_COLS];
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int j = 0; j < DOT_COLS; ++j) acc[r][j] = 0.f;
-    for (int v = v0 + lane; v < v1 + lane; v += 32 * DOT_AHEAD) {        // the same number of turns for all lanes
-        fetch(next, v + 32 * DOT_AHEAD);
+            for (int j = 0; j < DOT_COLS; ++j) acc[r][j] = 0.f;
+        for (int v = v0 + lane; v < v1 + lane; v += 32 * DOT_AHEAD) {    // the same number of turns for all lanes
+            const bool more = v + 32 * DOT_AHEAD < v1 + lane;
+            fetch(next, more ? unit : unit + stride, more ? v + 32 * DOT_AHEAD : v0 + lane);
 #pragma unroll
-        for (int u = 0; u < DOT_AHEAD; ++u) {
-            const int vu = v + 32 * u;
-            if (vu < v1 && cols > 0) {
-                const int g = vu * 16 / a.by_gs;
-                const float4 sw = __ldg(reinterpret_cast<const float4 *>(a.sW + (size_t)g * a.Kp + k0));
-                const float s[DOT_COLS] = {sw.x, sw.y, sw.z, sw.w};
+            for (int u = 0; u < DOT_AHEAD; ++u) {
+                const int vu = v + 32 * u;
+                if (vu < v1) {
+                    const int g = vu * 16 / a.by_gs;
+                    const float4 sw = __ldg(reinterpret_cast<const float4 *>(a.sW + (size_t)g * a.Kp + k0));
+                    const float s[DOT_COLS] = {sw.x, sw.y, sw.z, sw.w};
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const uint4 q = *reinterpret_cast<const uint4 *>(codes + r * a.Cp + vu * 16);
-                    const float sr = sx[r * a.G + g];
+                    for (int r = 0; r < R; ++r) {
+                        const uint4 q = *reinterpret_cast<const uint4 *>(codes + r * a.Cp + vu * 16);
+                        const float sr = sx[r * a.G + g];
 #pragma unroll
-                    for (int j = 0; j < DOT_COLS; ++j) {
-                        int d = __dp4a((int)q.x, (int)now[u][j].x, 0);
-                        d = __dp4a((int)q.y, (int)now[u][j].y, d);
-                        d = __dp4a((int)q.z, (int)now[u][j].z, d);
-                        d = __dp4a((int)q.w, (int)now[u][j].w, d);
-                        acc[r][j] = fmaf((float)d * sr, s[j], acc[r][j]);
+                        for (int j = 0; j < DOT_COLS; ++j) {
+                            int d = __dp4a((int)q.x, (int)now[u][j].x, 0);
+                            d = __dp4a((int)q.y, (int)now[u][j].y, d);
+                            d = __dp4a((int)q.z, (int)now[u][j].z, d);
+                            d = __dp4a((int)q.w, (int)now[u][j].w, d);
+                            acc[r][j] = fmaf((float)d * sr, s[j], acc[r][j]);
+                        }
                     }
                 }
-            }
 #pragma unroll
-            for (int j = 0; j < DOT_COLS; ++j) now[u][j] = next[u][j];
+                for (int j = 0; j < DOT_COLS; ++j) now[u][j] = next[u][j];
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = 0; j < DOT_COLS; ++j)
+#pragma unroll
+                for (int o = 16; o; o >>= 1) acc[r][j] += __shfl_xor_sync(0xffffffffu, acc[r][j], o);
+        // lane 2 r + p finishes columns 2 p and 2 p + 1 of row r
+        float f0 = 0.f, f1 = 0.f;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int p = 0; p < DOT_COLS / 2; ++p)
+                if (lane == 2 * r + p) { f0 = acc[r][2 * p]; f1 = acc[r][2 * p + 1]; }
+        if (a.parts == 1) {
+            if (lane < 2 * R) finish_pair(a.out, lane / 2, k0 + 2 * (lane & 1), f0, f1);
+        } else if (lane < 2 * R) {
+            float *mine = part + warp * R * DOT_COLS;
+            mine[2 * lane] = f0;
+            mine[2 * lane + 1] = f1;
         }
     }
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int j = 0; j < DOT_COLS; ++j)
-#pragma unroll
-            for (int o = 16; o; o >>= 1) acc[r][j] += __shfl_xor_sync(0xffffffffu, acc[r][j], o);
-    // lane 2 r + p finishes columns 2 p and 2 p + 1 of row r
-    float f0 = 0.f, f1 = 0.f;
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int p = 0; p < DOT_COLS / 2; ++p)
-            if (lane == 2 * r + p) { f0 = acc[r][2 * p]; f1 = acc[r][2 * p + 1]; }
     if (a.parts > 1) {
-        float *mine = part + warp * R * DOT_COLS;
-        if (lane < 2 * R) { mine[2 * lane] = f0; mine[2 * lane + 1] = f1; }
         __syncthreads();
-        if (seg == 0 && lane < 2 * R)
-            for (int p = 1; p < a.parts; ++p) {       // in order
+        const int k0 = ((int)blockIdx.x * DOT_WARPS + warp) / a.parts * DOT_COLS;
+        if (seg == 0 && lane < 2 * R && k0 < a.out.Kz) {
+            float f0 = 0.f, f1 = 0.f;
+            for (int p = 0; p < a.parts; ++p) {       // in order
                 f0 += part[(warp + p) * R * DOT_COLS + 2 * lane];
                 f1 += part[(warp + p) * R * DOT_COLS + 2 * lane + 1];
             }
+            finish_pair(a.out, lane / 2, k0 + 2 * (lane & 1), f0, f1);
+        }
     }
-    if (seg == 0 && lane < 2 * R) finish_pair(a.out, lane / 2, k0 + 2 * (lane & 1), f0, f1);
 }
 
 // How a call is laid out: orientation (1: rows of x on the lanes, 2: outputs, 3: pairs of CTAs with rows of x, 4: dot
@@ -1097,10 +1120,13 @@ Shape choose(const wfq_linear &l, int rows)
     const bool dot = rows <= DOT_MAX_ROWS && dot_smem(rows, l.Cp, l.G) <= DOT_SMEM_MAX;
     if (l.debug_shape && (dot || l.debug_shape / 1000 % 10 != 4))
         return Shape{l.debug_shape / 1000 % 10, l.debug_shape % 1000, l.debug_shape / 10000};
-    if (dot) return Shape{4, 4, 1};
     const int KB = (l.Cp / 32 + 3) / 4;
     Shape best{1, 64, 1};
     double best_cost = 1e300;
+    if (dot) {       // bytes at a rate that falls with the rows' arithmetic, less the tensor kernels' longer way in and out
+        best = Shape{4, 4, 1};
+        best_cost = (double)l.Kz * l.Cp / (rows <= 2 ? 5.0e6 : rows <= 4 ? 3.6e6 : 2.2e6) - 2.2;
+    }
     for (int orient = 1; orient <= 3; ++orient)
         for (int bn : {256, 128, 64, 32, 16})
             for (int split : {1, 2, 4, 8}) {
@@ -1224,7 +1250,9 @@ cudaError_t launch_dot(const wfq_linear &l, const void *x, long long ldx, const 
     const int quads = (l.Kz + DOT_COLS - 1) / DOT_COLS;
     a.parts = 1;
     while (a.parts < 8 && (long long)quads * a.parts < 16LL * l.sm_count && l.Cp / 16 / (2 * a.parts) >= 64) a.parts *= 2;
-    const int grid = (int)(((long long)quads * a.parts + DOT_WARPS - 1) / DOT_WARPS), smem = dot_smem(rows, l.Cp, l.G);
+    a.units = quads * a.parts;
+    const int smem = dot_smem(rows, l.Cp, l.G), ctas = (a.units + DOT_WARPS - 1) / DOT_WARPS;
+    const int grid = a.parts > 1 || ctas < 2 * l.sm_count ? ctas : 2 * l.sm_count;
     if (!x) return launch_dot_rows<int8_t>(a, grid, smem, stream, pdl);
     if (l.in_dtype == WFQ_F32) return launch_dot_rows<float>(a, grid, smem, stream, pdl);
     if (l.in_dtype == WFQ_F16) return launch_dot_rows<__half>(a, grid, smem, stream, pdl);
@@ -1335,7 +1363,7 @@ wfq_status_t run(wfq_linear *l, const void *x, long long ldx, int8_t *xq, float 
     o.vec = !misaligned(y, 16) && ldy * e % 16 == 0 && (!residual || (!misaligned(residual, 16) && ldr * e % 16 == 0));
 
     const bool dot = shape_for(*l, rows).orient == 4;
-    const bool quantize = x && !dot;
+    const bool quantize = x && !(dot && (long long)rows * l->Cp <= DOT_QUANTIZE_MAX);
     if (quantize) {
         RowsArgs a;
         a.x = x; a.ldx = ldx;
@@ -1356,7 +1384,7 @@ wfq_status_t run(wfq_linear *l, const void *x, long long ldx, int8_t *xq, float 
         if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) return WFQ_ERR_CUDA;
         if (cap == cudaStreamCaptureStatusNone) l->fresh = false;
     }
-    if (dot) return to_status(launch_dot(*l, x, ldx, xq, sx, rows, o, st, pdl));
+    if (dot) return to_status(launch_dot(*l, quantize ? nullptr : x, ldx, xq, sx, rows, o, st, pdl));
     return to_status(launch_product(*l, xq, sx, rows, o, st, pdl));
 }
 

@@ -172,6 +172,9 @@ __device__ __forceinline__ void tma_prefetch_l2_3d(const CUtensorMap *map, int c
                  : "memory");
 }
 
+// Asks for the line that holds *p to be brought into L2.
+__device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
 // Makes this thread's earlier shared-memory writes (generic proxy) visible to the
 // asynchronous proxy (TMA, tcgen05.mma operand reads).
 __device__ __forceinline__ void fence_proxy_async_smem()
