@@ -536,6 +536,9 @@ def _rows_of(x, C, what):
 
 
 def _empty(shape, dtype, device):
+    # with its strides given: a microsecond less than torch.empty
+    if len(shape) == 2:
+        return _torch.empty_strided(shape, (shape[1] or 1, 1), dtype=dtype, device=device)
     strides, n = [], 1
     for size in reversed(shape):
         strides.append(n)
@@ -544,13 +547,15 @@ def _empty(shape, dtype, device):
 
 
 def _call(index, fn, *args):
-    """fn(*args, stream) with device `index` current, on its current stream."""
+    """The library's fn(*args, stream) with device `index` current, on its current stream."""
     c = _torch._C
     if c._cuda_getDevice() == index:
-        fn(*args, c._cuda_getCurrentRawStream(index))
+        status = fn(*args, c._cuda_getCurrentRawStream(index))
     else:
         with _torch.cuda.device(index):
-            fn(*args, c._cuda_getCurrentRawStream(index))
+            status = fn(*args, c._cuda_getCurrentRawStream(index))
+    if status != WFQ_OK:
+        _check(status, fn.__name__)
 
 
 class QuantizedRows:
@@ -595,18 +600,18 @@ def rms_norm_quantize(x, gain, eps=1e-6, group_size=128, residual=None, out=None
     q = QuantizedRows(rows, C, group_size, device, shape)
     if residual is None:
         assert out is None, "out: only with a residual"
-        _call(index, wfq_rms_norm_quantize, x.data_ptr(), ldx, None, 0, gain.data_ptr(), eps, code, rows, C, group_size,
+        _call(index, (_lib or load()).wfq_rms_norm_quantize, x.data_ptr(), ldx, None, 0, gain.data_ptr(), eps, code, rows, C, group_size,
               None, 0, q._codes, q._scales)
         return q, x
     assert residual.shape == shape and residual.dtype is dtype and residual.get_device() == index, "residual"
     _, ldr = _rows_of(residual, C, "residual")
     if out is None:
-        h, ldh = _empty(shape, dtype, device), C
+        h, ldh = torch.empty_like(x) if ldx == C and x.is_contiguous() else _empty(shape, dtype, device), C
     else:
         h = out
         assert h.shape == shape and h.dtype is dtype and h.get_device() == index, "out"
         _, ldh = _rows_of(h, C, "out")
-    _call(index, wfq_rms_norm_quantize, x.data_ptr(), ldx, residual.data_ptr(), ldr, gain.data_ptr(), eps, code, rows, C,
+    _call(index, (_lib or load()).wfq_rms_norm_quantize, x.data_ptr(), ldx, residual.data_ptr(), ldr, gain.data_ptr(), eps, code, rows, C,
           group_size, h.data_ptr(), ldh, q._codes, q._scales)
     return q, h
 
@@ -619,14 +624,14 @@ def quantize_rows(x, group_size=128):
     assert code is not None, "x: fp32, fp16 or bf16"
     rows, ldx = _rows_of(x, C, "x")
     q = QuantizedRows(rows, C, group_size, x.device, x.shape)
-    _call(q.index, wfq_quantize_rows, x.data_ptr(), ldx, code, rows, C, group_size, q._codes, q._scales)
+    _call(q.index, (_lib or load()).wfq_quantize_rows, x.data_ptr(), ldx, code, rows, C, group_size, q._codes, q._scales)
     return q
 
 
 def dequantize_rows(q, dtype="f16"):
     """The values of QuantizedRows in "f32", "f16" or "bf16", shaped like the tensor they came from."""
     v = _empty(q.shape, _NAMED[dtype], q._buf.device)
-    _call(q.index, wfq_dequantize_rows, q._codes, q._scales, q.rows, q.C, q.group_size, _DTYPES[dtype], v.data_ptr(), q.C)
+    _call(q.index, (_lib or load()).wfq_dequantize_rows, q._codes, q._scales, q.rows, q.C, q.group_size, _DTYPES[dtype], v.data_ptr(), q.C)
     return v
 
 
@@ -654,7 +659,7 @@ class Linear:
         assert w.get_device() == self.index and w.dtype in _CODES
         assert w.shape == ((2 if self.gated else 1) * self.K, self.C)
         _, ldw = _rows_of(w, self.C, "w")
-        _call(self.index, wfq_linear_prepare_weights, self.lin, w.data_ptr(), ldw, _CODES[w.dtype])
+        _call(self.index, _lib.wfq_linear_prepare_weights, self.lin, w.data_ptr(), ldw, _CODES[w.dtype])
 
     def set_epilogue(self, bias=None, act=WFQ_ACT_NONE):
         """bias: fp32 CUDA tensor [K] ([2K] if gated) or None; kept alive by this object."""
@@ -682,7 +687,7 @@ class Linear:
         assert x.dtype is self._in and x.get_device() == self.index, "x"
         rows, ldx = _rows_of(x, self.C, "x")
         y, ldy, res, ldr = self._outputs(x.shape[:-1], residual, y)
-        _call(self.index, wfq_linear_forward, self.lin, x.data_ptr(), ldx, rows, res, ldr, y.data_ptr(), ldy)
+        _call(self.index, _lib.wfq_linear_forward, self.lin, x.data_ptr(), ldx, rows, res, ldr, y.data_ptr(), ldy)
         return y
 
     def forward_codes(self, q, residual=None, y=None):
@@ -690,7 +695,7 @@ class Linear:
         assert q.C == self.C and q.index == self.index, "q"
         assert q.group_size == self.gs or (q.groups == 1 and (self.gs == 0 or self.gs >= self.C)), "q: groups"
         y, ldy, res, ldr = self._outputs(q.shape[:-1], residual, y)
-        _call(self.index, wfq_linear_forward_codes, self.lin, q._codes, q._scales, q.rows, res, ldr, y.data_ptr(), ldy)
+        _call(self.index, _lib.wfq_linear_forward_codes, self.lin, q._codes, q._scales, q.rows, res, ldr, y.data_ptr(), ldy)
         return y
 
     def check_status(self):

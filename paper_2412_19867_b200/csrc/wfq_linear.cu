@@ -33,10 +33,13 @@ struct wfq_linear {
     int act = 0;
     int device = -1, sm_count = 0;
     int8_t *Wq = nullptr;                      // [Kz][Cp]
+    CUtensorMap tmap_w[2];                     // Wq in boxes of 64 and of 128 rows x 128 channels
+    bool tmap_w_ok[2] = {false, false};
     float *sW = nullptr;                       // [G][Kp], zero behind Kz
     int *status = nullptr;                     // int32[4]
     bool prepared = false;
-    bool fresh = false;                        // weights were written since the last launch that waited for them
+    bool fresh = false;                        // weights were written since the last product that waited for them
+    bool written_by_graph = false;             // a captured call writes them
     int8_t *xq = nullptr;                      // workspace: codes of up to max_rows rows
     float *sx = nullptr;
     int max_rows = 0;
@@ -121,7 +124,6 @@ struct MmaArgs {
     int *status;
     long long wait_cycles;
     int debug_skip_stage;
-    int early;                 // the weights may be read before the previous kernel has completed
     OutArgs out;
 };
 
@@ -725,7 +727,7 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         long long issued = 0;
         bool ok = true;
         for (int t = first; t < a.tiles && ok; t += stride) {
-            const int mt = t % a.MT, nt = t / a.MT;
+            const int a_row = t % a.MT * row_block + row_off, b_row = t / a.MT * BN + (PAIR ? rank * C::B_ROWS : 0);
             for (int kb = rg.kb0; kb < rg.kb1; ++kb) {
                 ok = wait<C>(ptx::smem_u32(&sh->empty[stage]), phase ^ 1u, ctx, kWaitSmemEmpty);
                 if (!ok) break;
@@ -735,12 +737,12 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                     if constexpr (PAIR) {      // the leader's barrier counts both CTAs' bytes
                         const uint32_t lead = ptx::map_rank(bar, 0);
                         if (rank == 0) ptx::mbar_arrive_expect_tx(bar, 2 * C::STAGE_BYTES);
-                        ptx::tma_load_2d_pair(dst, &tmA, lead, kb * BK, mt * row_block + row_off);
-                        ptx::tma_load_2d_pair(dst + A_BYTES, &tmB, lead, kb * BK, nt * BN + rank * C::B_ROWS);
+                        ptx::tma_load_2d_pair(dst, &tmA, lead, kb * BK, a_row);
+                        ptx::tma_load_2d_pair(dst + A_BYTES, &tmB, lead, kb * BK, b_row);
                     } else {
                         ptx::mbar_arrive_expect_tx(bar, C::STAGE_BYTES);
-                        ptx::tma_load_2d(dst, &tmA, bar, kb * BK, mt * BM);
-                        ptx::tma_load_2d(dst + A_BYTES, &tmB, bar, kb * BK, nt * BN);
+                        ptx::tma_load_2d(dst, &tmA, bar, kb * BK, a_row);
+                        ptx::tma_load_2d(dst + A_BYTES, &tmB, bar, kb * BK, b_row);
                     }
                 }
                 __syncwarp();
@@ -1165,15 +1167,18 @@ cudaError_t setup_variant()
 }
 
 template <int BN, bool SWAP, bool PAIR>
-cudaError_t launch_variant(const wfq_linear &l, MmaArgs &a, int grid, const int8_t *xq, int rows, cudaStream_t stream,
-                           bool pdl)
+cudaError_t launch_variant(wfq_linear &l, MmaArgs &a, int grid, const int8_t *xq, int rows, cudaStream_t stream)
 {
     a.cg = 1;
     if (BK % l.gs == 0) a.cg = BK / l.gs < Cfg<BN, SWAP, PAIR>::CG_MAX ? BK / l.gs : Cfg<BN, SWAP, PAIR>::CG_MAX;
     a.slots = Cfg<BN, SWAP, PAIR>::PIECES / a.cg;
-    CUtensorMap tx, tw;
-    if (!encode_codes(&tx, xq, l.Cp, rows, SWAP ? BN : BM) || !encode_codes(&tw, l.Wq, l.Cp, l.Kz, SWAP ? BM : Cfg<BN, SWAP, PAIR>::B_ROWS))
-        return cudaErrorInvalidValue;
+    constexpr int w_rows = SWAP ? BM : Cfg<BN, SWAP, PAIR>::B_ROWS;
+    constexpr int w_map = w_rows == 128 ? 1 : 0;
+    static_assert(w_rows == 128 || w_rows == 64, "rows of a box of weights");
+    CUtensorMap tx;
+    if (!l.tmap_w_ok[w_map]) l.tmap_w_ok[w_map] = encode_codes(&l.tmap_w[w_map], l.Wq, l.Cp, l.Kz, w_rows);
+    if (!l.tmap_w_ok[w_map] || !encode_codes(&tx, xq, l.Cp, rows, SWAP ? BN : BM)) return cudaErrorInvalidValue;
+    const CUtensorMap &tw = l.tmap_w[w_map];
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(THREADS);
@@ -1181,10 +1186,8 @@ cudaError_t launch_variant(const wfq_linear &l, MmaArgs &a, int grid, const int8
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     int n = 0;
-    if (pdl) {
-        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[n++].val.programmaticStreamSerializationAllowed = 1;
-    }
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
     if (PAIR || a.split > 1) {
         attr[n].id = cudaLaunchAttributeClusterDimension;
         attr[n].val.clusterDim.x = PAIR ? 2u : (unsigned)a.split;
@@ -1197,7 +1200,7 @@ cudaError_t launch_variant(const wfq_linear &l, MmaArgs &a, int grid, const int8
 }
 
 template <int R, typename T>
-cudaError_t launch_dot_kernel(const DotArgs &a, int grid, int smem, cudaStream_t stream, bool pdl)
+cudaError_t launch_dot_kernel(const DotArgs &a, int grid, int smem, cudaStream_t stream)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
@@ -1208,16 +1211,16 @@ cudaError_t launch_dot_kernel(const DotArgs &a, int grid, int smem, cudaStream_t
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = pdl ? 1 : 0;
+    cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, linear_dot_kernel<R, T>, a);
 }
 template <typename T>
-cudaError_t launch_dot_rows(const DotArgs &a, int grid, int smem, cudaStream_t stream, bool pdl)
+cudaError_t launch_dot_rows(const DotArgs &a, int grid, int smem, cudaStream_t stream)
 {
-    if (a.rows <= 1) return launch_dot_kernel<1, T>(a, grid, smem, stream, pdl);
-    if (a.rows <= 2) return launch_dot_kernel<2, T>(a, grid, smem, stream, pdl);
-    if (a.rows <= 4) return launch_dot_kernel<4, T>(a, grid, smem, stream, pdl);
-    return launch_dot_kernel<8, T>(a, grid, smem, stream, pdl);
+    if (a.rows <= 1) return launch_dot_kernel<1, T>(a, grid, smem, stream);
+    if (a.rows <= 2) return launch_dot_kernel<2, T>(a, grid, smem, stream);
+    if (a.rows <= 4) return launch_dot_kernel<4, T>(a, grid, smem, stream);
+    return launch_dot_kernel<8, T>(a, grid, smem, stream);
 }
 template <typename T>
 cudaError_t setup_dot()
@@ -1235,7 +1238,7 @@ cudaError_t setup_dot()
 
 // x: values in the layer's input type, or null with codes and scales.
 cudaError_t launch_dot(const wfq_linear &l, const void *x, long long ldx, const int8_t *xq, const float *sx, int rows,
-                       const OutArgs &out, cudaStream_t stream, bool pdl)
+                       const OutArgs &out, cudaStream_t stream, bool early)
 {
     DotArgs a;
     a.x = x; a.ldx = ldx;
@@ -1244,7 +1247,7 @@ cudaError_t launch_dot(const wfq_linear &l, const void *x, long long ldx, const 
     a.C = l.C; a.Cp = l.Cp; a.G = l.G; a.rows = rows; a.Kp = l.Kp;
     a.by_gs = FastDiv(l.gs);
     a.by_vectors = FastDiv(l.Cp / 8);
-    a.early = pdl;
+    a.early = early;
     a.out = out;
     // as many warps to a column as give every SM two CTAs, but a lane two vectors at least
     const int quads = (l.Kz + DOT_COLS - 1) / DOT_COLS;
@@ -1253,10 +1256,10 @@ cudaError_t launch_dot(const wfq_linear &l, const void *x, long long ldx, const 
     a.units = quads * a.parts;
     const int smem = dot_smem(rows, l.Cp, l.G), ctas = (a.units + DOT_WARPS - 1) / DOT_WARPS;
     const int grid = a.parts > 1 || ctas < 2 * l.sm_count ? ctas : 2 * l.sm_count;
-    if (!x) return launch_dot_rows<int8_t>(a, grid, smem, stream, pdl);
-    if (l.in_dtype == WFQ_F32) return launch_dot_rows<float>(a, grid, smem, stream, pdl);
-    if (l.in_dtype == WFQ_F16) return launch_dot_rows<__half>(a, grid, smem, stream, pdl);
-    return launch_dot_rows<__nv_bfloat16>(a, grid, smem, stream, pdl);
+    if (!x) return launch_dot_rows<int8_t>(a, grid, smem, stream);
+    if (l.in_dtype == WFQ_F32) return launch_dot_rows<float>(a, grid, smem, stream);
+    if (l.in_dtype == WFQ_F16) return launch_dot_rows<__half>(a, grid, smem, stream);
+    return launch_dot_rows<__nv_bfloat16>(a, grid, smem, stream);
 }
 
 const Shape shape_for(wfq_linear &l, int rows)
@@ -1269,7 +1272,7 @@ const Shape shape_for(wfq_linear &l, int rows)
 }
 
 cudaError_t launch_product(wfq_linear &l, const int8_t *xq, const float *sx, int rows, const OutArgs &out,
-                           cudaStream_t stream, bool pdl)
+                           cudaStream_t stream)
 {
     const Shape sp = shape_for(l, rows);
     MmaArgs a;
@@ -1289,21 +1292,20 @@ cudaError_t launch_product(wfq_linear &l, const int8_t *xq, const float *sx, int
     a.status = l.status;
     a.wait_cycles = l.wait_cycles;
     a.debug_skip_stage = l.debug_skip_stage;
-    a.early = 0;
     a.out = out;
     const int at_once = pair ? l.sm_count / 2 : l.sm_count;
     const int grid = sp.split > 1 ? a.tiles * sp.split : (a.tiles < at_once ? a.tiles : at_once) * (pair ? 2 : 1);
     if (swap) {
-        if (sp.bn == 16) return launch_variant<16, true, false>(l, a, grid, xq, rows, stream, pdl);
-        if (sp.bn == 32) return launch_variant<32, true, false>(l, a, grid, xq, rows, stream, pdl);
-        return launch_variant<64, true, false>(l, a, grid, xq, rows, stream, pdl);
+        if (sp.bn == 16) return launch_variant<16, true, false>(l, a, grid, xq, rows, stream);
+        if (sp.bn == 32) return launch_variant<32, true, false>(l, a, grid, xq, rows, stream);
+        return launch_variant<64, true, false>(l, a, grid, xq, rows, stream);
     }
     if (pair) {
-        if (sp.bn == 128) return launch_variant<128, false, true>(l, a, grid, xq, rows, stream, pdl);
-        return launch_variant<256, false, true>(l, a, grid, xq, rows, stream, pdl);
+        if (sp.bn == 128) return launch_variant<128, false, true>(l, a, grid, xq, rows, stream);
+        return launch_variant<256, false, true>(l, a, grid, xq, rows, stream);
     }
-    if (sp.bn == 64) return launch_variant<64, false, false>(l, a, grid, xq, rows, stream, pdl);
-    return launch_variant<128, false, false>(l, a, grid, xq, rows, stream, pdl);
+    if (sp.bn == 64) return launch_variant<64, false, false>(l, a, grid, xq, rows, stream);
+    return launch_variant<128, false, false>(l, a, grid, xq, rows, stream);
 }
 
 bool known(wfq_dtype_t t) { return t == WFQ_F32 || t == WFQ_F16 || t == WFQ_BF16; }
@@ -1373,19 +1375,18 @@ wfq_status_t run(wfq_linear *l, const void *x, long long ldx, int8_t *xq, float 
         a.scale_pitch = (rows + 127LL) / 128 * 128;
         if (launch_rows(a, l->in_dtype, st, true) != cudaSuccess) return WFQ_ERR_CUDA;
     }
-    // The product's launch may begin before the kernel in front of it has ended, and fetches weights then.  The row
-    // quantizer lets it begin only after its own wait for what was in front of it, fresh weights too; without it, weights
-    // that were written since are waited for by an ordinary launch.  Under capture the launch is only recorded, and the
-    // weights stay fresh.
-    bool pdl = true;
-    if (l->fresh && !quantize) {
-        pdl = false;
+    // The product's launch may begin before the kernel in front of it has ended, and may fetch weights then if that cannot
+    // be the one that writes them: the row quantizer lets it begin only after its own wait for what was in front of it; and
+    // weights that were written since the last product are waited for.  Under capture the launch is only recorded, and the
+    // weights stay fresh; where a graph writes them, its replays do so unseen.
+    const bool early = quantize || !(l->fresh || l->written_by_graph);
+    if (l->fresh) {
         cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
         if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) return WFQ_ERR_CUDA;
         if (cap == cudaStreamCaptureStatusNone) l->fresh = false;
     }
-    if (dot) return to_status(launch_dot(*l, quantize ? nullptr : x, ldx, xq, sx, rows, o, st, pdl));
-    return to_status(launch_product(*l, xq, sx, rows, o, st, pdl));
+    if (dot) return to_status(launch_dot(*l, quantize ? nullptr : x, ldx, xq, sx, rows, o, st, early));
+    return to_status(launch_product(*l, xq, sx, rows, o, st));
 }
 
 }  // namespace
@@ -1484,6 +1485,9 @@ wfq_status_t wfq_linear_prepare_weights(wfq_linear_t *l, const void *w_dev, long
     a.gs = l->gs; a.G = l->G;
     a.scale_pitch = l->Kp;
     a.half = l->gated ? l->K : 0;
+    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) return WFQ_ERR_CUDA;
+    if (cap != cudaStreamCaptureStatusNone) l->written_by_graph = true;
     l->fresh = true;
     if (launch_rows(a, dtype, st, false) != cudaSuccess) { l->prepared = false; return WFQ_ERR_CUDA; }
     l->prepared = true;

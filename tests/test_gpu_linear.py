@@ -259,3 +259,27 @@ def test_starved_product_ends(shape, stage):
     layer = _layer(C=2048, K=200, rows=100)
     assert torch.equal(layer.forward(x), want)
     layer.check_status()
+
+
+@pytest.mark.parametrize("rows", [1, 4, 20, 200])
+def test_weights_written_by_a_graph(rows):
+    """A graph that prepares the weights, and products behind its replays, inside the graph and outside."""
+    layer = _layer(C=1024, K=512, gs=128, rows=rows)
+    w = _rand((512, 1024), torch.float16, 20, 0.02)
+    q = b.quantize_rows(_rand((rows, 1024), torch.float16, rows), 128)
+    layer.prepare(w)
+    layer.forward_codes(q)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.prepare(w)
+        inside = layer.forward_codes(q)
+    for seed in range(21, 27):
+        w.copy_(_rand((512, 1024), torch.float16, seed, 0.02))
+        graph.replay()
+        outside = layer.forward_codes(q)
+        torch.cuda.synchronize()
+        fresh = _layer(C=1024, K=512, gs=128, rows=rows)
+        fresh.prepare(w)
+        want = fresh.forward_codes(q)
+        assert torch.equal(inside, want) and torch.equal(outside, want)
