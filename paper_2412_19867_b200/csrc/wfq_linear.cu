@@ -14,6 +14,12 @@
 //   warps 4-11  epilogue: int32 sums to fp32, times the scales, into registers; then bias, activation, gate, residual
 // With few tiles a cluster of up to eight CTAs shares one: each takes a range of the channels, the partial sums are
 // added in rank order through distributed shared memory, each CTA for a share of the columns.
+// What bounds it.  Short groups: the epilogue's arithmetic, a conversion and two products per group sum.  2048 x 8192 ->
+// 2048 in groups of 128 on pairs (one tile per pair of CTAs): 61 us, 1.1 POPS; a piece of 128 x 256 sums takes the eight
+// epilogue warps 1200 cycles, of which the conversions are 300, one product 250, the loads 160, against 512 of its MMAs.
+// Long groups: the MMAs at the clock that the power limit leaves; 8192 x 4096 -> 8192 with one scale per row 178 us,
+// 3.1 POPS of the 4.6 that MMAs without loads reach.  Few rows: the weights' bytes; 24 x 4096 -> 32768 30 us, 4.5 TB/s,
+// where 256 tiles on 148 SMs leave the second round half empty.
 // Every wait is bounded; on expiry the CTA records where, stops, drains and frees TMEM.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -269,9 +275,11 @@ __device__ __forceinline__ void activate_all(float (&z)[N], int act)
 
 // The sums of an epilogue warp, 32 rows of TMEM lanes x CW columns.  Where there are many columns (!SWAP) a thread has four
 // rows, lane / 4 + 8 q, and every fourth pair of columns, 8 j + 2 (lane % 4): a column scale is then read from shared
-// memory by four threads instead of by all 32.  With a row per thread the reads return CW floats to every lane, 1024 cycles
-// of the SM's 128 bytes a clock for a piece of 128 x 256, which bounded the kernel whatever the arithmetic
-// (4096 channels in groups of 128, 1050 cycles a piece of 128 x 128).  With SWAP (few columns) a thread has one row.
+// memory by eight lanes instead of by all 32.  With a row per thread the reads return CW floats to
+// every lane, 1024 cycles of the SM's 128 bytes a clock for a piece of 128 x 256, which then takes 1700 cycles instead of
+// 1300 with its wait.  Sums that start from the bit pattern of 1.5 * 2^23, so that they need no conversion, cost more in
+// writing the pattern back (2000 to 2500 cycles); sixteen epilogue warps with half the columns each are 10 % slower.  With
+// SWAP (few columns) a thread has one row.
 template <int CW, bool SWAP> struct Sums;
 template <int CW> struct Sums<CW, false> {
     float2 v[4][CW / 8];         // [q][j]
@@ -719,94 +727,94 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     ptx::grid_launch_dependents();
 
     if (warp < FIRST_EPI_WARP) {
-    if constexpr (C::MOVE_REGS) ptx::fewer_registers<56>();
-    if (warp == 0) {
-        // ---------------- TMA producer ----------------
-        int stage = 0;
-        uint32_t phase = 0;
-        long long issued = 0;
-        bool ok = true;
-        for (int t = first; t < a.tiles && ok; t += stride) {
-            const int a_row = t % a.MT * row_block + row_off, b_row = t / a.MT * BN + (PAIR ? rank * C::B_ROWS : 0);
-            for (int kb = rg.kb0; kb < rg.kb1; ++kb) {
-                ok = wait<C>(ptx::smem_u32(&sh->empty[stage]), phase ^ 1u, ctx, kWaitSmemEmpty);
-                if (!ok) break;
-                if (ptx::elect_one() && !(blockIdx.x == 0 && issued == a.debug_skip_stage)) {
-                    const uint32_t bar = ptx::smem_u32(&sh->full[stage]);
-                    const uint32_t dst = ptx::smem_u32(tiles + (size_t)stage * C::STAGE_BYTES);
-                    if constexpr (PAIR) {      // the leader's barrier counts both CTAs' bytes
-                        const uint32_t lead = ptx::map_rank(bar, 0);
-                        if (rank == 0) ptx::mbar_arrive_expect_tx(bar, 2 * C::STAGE_BYTES);
-                        ptx::tma_load_2d_pair(dst, &tmA, lead, kb * BK, a_row);
-                        ptx::tma_load_2d_pair(dst + A_BYTES, &tmB, lead, kb * BK, b_row);
-                    } else {
-                        ptx::mbar_arrive_expect_tx(bar, C::STAGE_BYTES);
-                        ptx::tma_load_2d(dst, &tmA, bar, kb * BK, a_row);
-                        ptx::tma_load_2d(dst + A_BYTES, &tmB, bar, kb * BK, b_row);
+        if constexpr (C::MOVE_REGS) ptx::fewer_registers<56>();
+        if (warp == 0) {
+            // ---------------- TMA producer ----------------
+            int stage = 0;
+            uint32_t phase = 0;
+            long long issued = 0;
+            bool ok = true;
+            for (int t = first; t < a.tiles && ok; t += stride) {
+                const int a_row = t % a.MT * row_block + row_off, b_row = t / a.MT * BN + (PAIR ? rank * C::B_ROWS : 0);
+                for (int kb = rg.kb0; kb < rg.kb1; ++kb) {
+                    ok = wait<C>(ptx::smem_u32(&sh->empty[stage]), phase ^ 1u, ctx, kWaitSmemEmpty);
+                    if (!ok) break;
+                    if (ptx::elect_one() && !(blockIdx.x == 0 && issued == a.debug_skip_stage)) {
+                        const uint32_t bar = ptx::smem_u32(&sh->full[stage]);
+                        const uint32_t dst = ptx::smem_u32(tiles + (size_t)stage * C::STAGE_BYTES);
+                        if constexpr (PAIR) {      // the leader's barrier counts both CTAs' bytes
+                            const uint32_t lead = ptx::map_rank(bar, 0);
+                            if (rank == 0) ptx::mbar_arrive_expect_tx(bar, 2 * C::STAGE_BYTES);
+                            ptx::tma_load_2d_pair(dst, &tmA, lead, kb * BK, a_row);
+                            ptx::tma_load_2d_pair(dst + A_BYTES, &tmB, lead, kb * BK, b_row);
+                        } else {
+                            ptx::mbar_arrive_expect_tx(bar, C::STAGE_BYTES);
+                            ptx::tma_load_2d(dst, &tmA, bar, kb * BK, a_row);
+                            ptx::tma_load_2d(dst + A_BYTES, &tmB, bar, kb * BK, b_row);
+                        }
                     }
+                    __syncwarp();
+                    ++issued;
+                    if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
                 }
-                __syncwarp();
-                ++issued;
-                if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
             }
-        }
-        if (!ok || sh->abort) {      // give copies in flight a bounded time to land
-            int s = stage;
-            uint32_t ph = phase;
-            const long long n = issued < C::STAGES ? issued : C::STAGES;
-            for (long long i = 0; i < n; ++i) {
-                if (--s < 0) { s = C::STAGES - 1; ph ^= 1u; }
-                drain(ptx::smem_u32(&sh->full[s]), ph);
-            }
-        }
-    } else if (warp == 1 && rank_issues) {
-        // ---------------- MMA issuer ----------------
-        const uint32_t tiles_lo = ptx::smem_desc_sw128_lo(ptx::smem_u32(tiles));
-        if (a.gsteps % 4 == 0 || a.gsteps >= a.steps) issue<BN, SWAP, PAIR, 4>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
-        else if (a.gsteps == 2) issue<BN, SWAP, PAIR, 2>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
-        else if (a.gsteps == 1) issue<BN, SWAP, PAIR, 1>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
-        else issue<BN, SWAP, PAIR, 0>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
-    } else if (warp == 2) {
-        // ---------------- scale loader ----------------
-        const uint32_t scale_bar = ptx::smem_u32(PAIR ? &sh->scale_free[0] : &sh->slot_free[0]);
-        int slot = 0;
-        uint32_t sphase = 0;
-        long long issued = 0;
-        bool ok = true;
-        for (int t = first; t < a.tiles && ok; t += stride) {
-            const int mt = t % a.MT, nt = t / a.MT;
-            // the second CTA of a pair may have no rows: it then reads scales that it does not use
-            const long long row0 = min((long long)mt * row_block + row_off, a.row_pitch - BM);
-            for (int q0 = 0; q0 < rg.np; q0 += a.cg) {
-                const int n = min(a.cg, rg.np - q0);
-                ok = wait<C>(scale_bar + 8u * slot, sphase ^ 1u, ctx, kWaitScaleEmpty);
-                if (!ok) break;
-                const uint32_t bar = ptx::smem_u32(&sh->acc_full[slot]);
-                const uint32_t dst = ptx::smem_u32(scales + (size_t)slot * a.cg * C::GROUP_SCALE_FLOATS);
-                if (ptx::elect_one()) ptx::mbar_arrive_expect_tx(bar, (uint32_t)(n * C::GROUP_SCALE_FLOATS * 4));
-                __syncwarp();
-                if (lane < 8 && (lane & 3) < n) {      // lane j: row scales of piece j, lane 4 + j: column scales
-                    const int j = lane & 3;
-                    const long long g = rg.g0 + q0 + j;
-                    const uint32_t d = dst + (uint32_t)(j * C::GROUP_SCALE_FLOATS * 4);
-                    if (lane < 4) ptx::bulk_load(d, a.row_scale + g * a.row_pitch + row0, BM * 4, bar);
-                    else ptx::bulk_load(d + BM * 4, a.col_scale + g * a.col_pitch + nt * BN, BN * 4, bar);
+            if (!ok || sh->abort) {      // give copies in flight a bounded time to land
+                int s = stage;
+                uint32_t ph = phase;
+                const long long n = issued < C::STAGES ? issued : C::STAGES;
+                for (long long i = 0; i < n; ++i) {
+                    if (--s < 0) { s = C::STAGES - 1; ph ^= 1u; }
+                    drain(ptx::smem_u32(&sh->full[s]), ph);
                 }
-                __syncwarp();
-                ++issued;
-                if (++slot == a.slots) { slot = 0; sphase ^= 1u; }
+            }
+        } else if (warp == 1 && rank_issues) {
+            // ---------------- MMA issuer ----------------
+            const uint32_t tiles_lo = ptx::smem_desc_sw128_lo(ptx::smem_u32(tiles));
+            if (a.gsteps % 4 == 0 || a.gsteps >= a.steps) issue<BN, SWAP, PAIR, 4>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
+            else if (a.gsteps == 2) issue<BN, SWAP, PAIR, 2>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
+            else if (a.gsteps == 1) issue<BN, SWAP, PAIR, 1>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
+            else issue<BN, SWAP, PAIR, 0>(sh, tiles_lo, tmem_base, a, rg, ctx, first, stride);
+        } else if (warp == 2) {
+            // ---------------- scale loader ----------------
+            const uint32_t scale_bar = ptx::smem_u32(PAIR ? &sh->scale_free[0] : &sh->slot_free[0]);
+            int slot = 0;
+            uint32_t sphase = 0;
+            long long issued = 0;
+            bool ok = true;
+            for (int t = first; t < a.tiles && ok; t += stride) {
+                const int mt = t % a.MT, nt = t / a.MT;
+                // the second CTA of a pair may have no rows: it then reads scales that it does not use
+                const long long row0 = min((long long)mt * row_block + row_off, a.row_pitch - BM);
+                for (int q0 = 0; q0 < rg.np; q0 += a.cg) {
+                    const int n = min(a.cg, rg.np - q0);
+                    ok = wait<C>(scale_bar + 8u * slot, sphase ^ 1u, ctx, kWaitScaleEmpty);
+                    if (!ok) break;
+                    const uint32_t bar = ptx::smem_u32(&sh->acc_full[slot]);
+                    const uint32_t dst = ptx::smem_u32(scales + (size_t)slot * a.cg * C::GROUP_SCALE_FLOATS);
+                    if (ptx::elect_one()) ptx::mbar_arrive_expect_tx(bar, (uint32_t)(n * C::GROUP_SCALE_FLOATS * 4));
+                    __syncwarp();
+                    if (lane < 8 && (lane & 3) < n) {      // lane j: row scales of piece j, lane 4 + j: column scales
+                        const int j = lane & 3;
+                        const long long g = rg.g0 + q0 + j;
+                        const uint32_t d = dst + (uint32_t)(j * C::GROUP_SCALE_FLOATS * 4);
+                        if (lane < 4) ptx::bulk_load(d, a.row_scale + g * a.row_pitch + row0, BM * 4, bar);
+                        else ptx::bulk_load(d + BM * 4, a.col_scale + g * a.col_pitch + nt * BN, BN * 4, bar);
+                    }
+                    __syncwarp();
+                    ++issued;
+                    if (++slot == a.slots) { slot = 0; sphase ^= 1u; }
+                }
+            }
+            if (!ok || sh->abort) {
+                int s = slot;
+                uint32_t ph = sphase;
+                const long long n = issued < a.slots ? issued : a.slots;
+                for (long long i = 0; i < n; ++i) {
+                    if (--s < 0) { s = a.slots - 1; ph ^= 1u; }
+                    drain(ptx::smem_u32(&sh->acc_full[s]), ph);
+                }
             }
         }
-        if (!ok || sh->abort) {
-            int s = slot;
-            uint32_t ph = sphase;
-            const long long n = issued < a.slots ? issued : a.slots;
-            for (long long i = 0; i < n; ++i) {
-                if (--s < 0) { s = a.slots - 1; ph ^= 1u; }
-                drain(ptx::smem_u32(&sh->acc_full[s]), ph);
-            }
-        }
-    }
     } else {
         // ---------------- epilogue ----------------
         if constexpr (C::MOVE_REGS) ptx::more_registers<216>();

@@ -87,20 +87,20 @@ def linear(codes, scales, wcodes, wscales, gs, bias=None, act="none", gated=Fals
     groups = edges(C, gs)
     z = torch.zeros((codes.shape[0], wcodes.shape[0]), dtype=torch.float64)
     size = torch.zeros_like(z)
-    terms = 0
+    unit = 16 if len(codes) <= 8 else 128              # channels that are summed in 32-bit integers at least
     for g, (lo, hi) in enumerate(groups):
-        # A group may be summed in parts that begin and end at multiples of 128 channels (several CTAs, or pieces of a
-        # long group); each part is rounded on its own, and with s = a + b and a, b of opposite signs |a| + |b| is any
-        # multiple of |s|.  So the size of a term is the sum of its smallest parts' magnitudes, which bounds the
+        # A group may be summed in parts that begin and end at multiples of `unit` channels (several CTAs, or
+        # several lanes for a few rows); each part is rounded on its own, and with s = a + b and a, b of opposite signs
+        # |a| + |b| is any multiple of |s|.  So the size of a term is the sum of its smallest parts' magnitudes, which bounds the
         # magnitudes of any larger ones: |a + b| <= |a| + |b|.
-        cuts = sorted({lo, hi} | set(range(-(-lo // 128) * 128, hi, 128)))
+        cuts = sorted({lo, hi} | set(range(-(-lo // unit) * unit, hi, unit)))
         for i, j in zip(cuts, cuts[1:]):
             t = (codes[:, i:j] @ wcodes[:, i:j].T) * scales[:, g:g + 1] * wscales[:, g][None]
             z += t
             size += t.abs()
-            terms += 1
-    # per term: conversion, a row scale of 22 bits, two products; then the additions, eight of them between CTAs
-    err = size * (6 + terms + 8) * U32
+    # per term: conversion and two products; then the additions: of a CTA's groups, or of a lane's parts, one in 32, and
+    # eight between CTAs or warps, five between lanes
+    err = size * (3 + max(len(groups), C / 512 + 1) + 13) * U32
     if bias is not None:
         z = z + bias.double().cpu()
         err = err + z.abs() * U32
