@@ -68,6 +68,7 @@ constexpr int A_BYTES = BM * BK;
 constexpr int EPI_WARPS = 8;
 constexpr int FIRST_EPI_WARP = 4;
 constexpr int PATCH_PITCH = 40;                                  // floats; 32 columns of z on their way out
+constexpr int RESIDUAL_BYTES = 8 * 32 * 16;                      // a warp's residual on its way in: eight 16-byte pieces a lane
 constexpr int THREADS = 32 * (FIRST_EPI_WARP + EPI_WARPS);
 
 struct Shared {
@@ -84,8 +85,8 @@ struct Cfg {
     static_assert(!(SWAP && PAIR), "pairs: rows of x on the lanes");
     static constexpr int B_ROWS = PAIR ? BN / 2 : BN;             // of the columns' operand in this CTA
     static constexpr int STAGE_BYTES = A_BYTES + B_ROWS * BK;
-    static constexpr int STAGES = STAGE_BYTES > 24 * 1024 ? 5 : STAGE_BYTES > 20 * 1024 ? (SWAP ? 8 : 7) : 9;
-    static constexpr int PATCH_BYTES = SWAP ? 0 : 32 * PATCH_PITCH * 4;           // of one epilogue warp
+    static constexpr int STAGES = STAGE_BYTES > 24 * 1024 ? 4 : STAGE_BYTES > 20 * 1024 ? (SWAP ? 8 : 5) : 9;
+    static constexpr int PATCH_BYTES = SWAP ? 0 : 32 * PATCH_PITCH * 4 + RESIDUAL_BYTES;      // of one epilogue warp
     // Pieces in tensor memory at a time, with their scales: chunks of one (of up to CG_MAX short groups) in as many slots
     // as that gives.  The scales of a slot are asked for when it is free; with two slots whatever the number of columns
     // that took longer than a stage of weights (24 rows, 4096 -> 16384 gated: 0.6 us per 128 channels).
@@ -195,51 +196,34 @@ __device__ __forceinline__ void finish_pair(const OutArgs &o, int r, int k, floa
     }
 }
 
-// N (4 or 8) consecutive values of y or the residual at once, aligned to their size up to 16 bytes.
-template <int N> struct Packed { uint32_t w[N]; };      // 16-bit types: the first half of it
+// y += n (4 or 8) values of the residual from 16-byte pieces in shared memory, `next` floats apart.
 template <int N>
-__device__ __forceinline__ Packed<N> load_packed(const void *p, long long i, int dtype)
+__device__ __forceinline__ void add_residual(float (&y)[N], const float *piece, int next, int dtype)
 {
-    Packed<N> r;
+    const uint4 u = *reinterpret_cast<const uint4 *>(piece);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
     if (dtype == WFQ_F32) {
-        const uint4 *q = reinterpret_cast<const uint4 *>(static_cast<const float *>(p) + i);
 #pragma unroll
-        for (int e = 0; e < N / 4; ++e) {
-            const uint4 u = q[e];
-            r.w[4 * e] = u.x; r.w[4 * e + 1] = u.y; r.w[4 * e + 2] = u.z; r.w[4 * e + 3] = u.w;
-        }
-    } else {
-        const uint2 *q = reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p) + i);
+        for (int i = 0; i < 4; ++i) y[i] += __uint_as_float(w[i]);
         if constexpr (N == 8) {
-            const uint4 u = *reinterpret_cast<const uint4 *>(q);
-            r.w[0] = u.x; r.w[1] = u.y; r.w[2] = u.z; r.w[3] = u.w;
-        } else {
-            const uint2 u = *q;
-            r.w[0] = u.x; r.w[1] = u.y;
+            const float4 v = *reinterpret_cast<const float4 *>(piece + next);
+            y[4] += v.x; y[5] += v.y; y[6] += v.z; y[7] += v.w;
         }
-    }
-    return r;
-}
-template <int N>
-__device__ __forceinline__ void add_packed(float (&y)[N], const Packed<N> &r, int dtype)
-{
-    if (dtype == WFQ_F32) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) y[i] += __uint_as_float(r.w[i]);
     } else if (dtype == WFQ_F16) {
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&r.w[i]));
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
             y[2 * i] += f.x; y[2 * i + 1] += f.y;
         }
     } else {
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) {
-            y[2 * i] += __uint_as_float(r.w[i] << 16);
-            y[2 * i + 1] += __uint_as_float(r.w[i] & 0xffff0000u);
+            y[2 * i] += __uint_as_float(w[i] << 16);
+            y[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
         }
     }
 }
+// N (4 or 8) consecutive values of y, aligned to their size up to 16 bytes.
 template <int N>
 __device__ __forceinline__ void store_packed(void *p, long long i, const float (&y)[N], int dtype)
 {
@@ -369,6 +353,34 @@ __device__ __forceinline__ void promote(uint32_t taddr, float rs, const float *c
 // A warp's 32 rows from row0 on, CW columns of z from column k0 on: 32 at a time through the warp's
 // patch of shared memory, so that lanes write neighbouring pieces of a row.  The pitch of 40 floats keeps the 8-byte writes
 // of sixteen lanes on different banks; reads of eight lanes are 16 bytes of two rows, of which one takes its upper half first.
+//
+// The residual comes in by asynchronous copies, each lane's own pieces (16 or 8 bytes; two of 16 for eight fp32 values) of
+// 32 columns at a time: the first 32 columns are asked for before the sums are formed, with 16-bit types the second, too.
+// Loaded where it is added it cost a memory latency per step, 16 us of 44 for 4096 x 128 -> 4096 bf16; held in registers
+// meanwhile it costs the promotion spills.
+template <int CW>
+__device__ __forceinline__ void ask_residual(const OutArgs &o, uint32_t buffer, int lane, int row0, int k0, int h)
+{
+    const int k = k0 + h + 8 * (lane % 4), j = o.gated ? k / 2 : k, elem = o.dtype == WFQ_F32 ? 4 : 2;
+    const int bytes = (o.gated ? 4 : 8) * elem;
+    if (o.vec && h < CW && k + 8 <= o.Kz) {
+        // 16-bit types: the other half of the buffer for every other 32 columns; fp32: all of it
+        const uint32_t dst = buffer + (elem == 2 && h % 64 ? 4u * 512u : 0u) + 16u * lane;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const long long r = row0 + 8 * q + lane / 4;
+            if (r >= o.R) break;
+            const char *src = static_cast<const char *>(o.residual) + (r * o.ldr + j) * elem;
+            if (bytes == 8) {
+                ptx::copy_async8(dst + 512u * q, src);
+            } else {
+                ptx::copy_async16(dst + 512u * q, src);
+                if (bytes == 32) ptx::copy_async16(dst + 512u * (4 + q), src + 16);
+            }
+        }
+    }
+    ptx::copy_async_commit();
+}
 template <int CW>
 __device__ __forceinline__ void finish_rows(const OutArgs &o, float *patch, int lane, int row0, int k0,
                                             const Sums<CW, false> &sums)
@@ -376,6 +388,8 @@ __device__ __forceinline__ void finish_rows(const OutArgs &o, float *patch, int 
     constexpr int COLS = 32, PITCH = PATCH_PITCH, PIECES = COLS / 8;      // pieces of eight columns
     constexpr int ROWS = 32 / PIECES;                             // rows per step
     const int piece = lane % PIECES, r_in = lane / PIECES;
+    float *residual = patch + 32 * PATCH_PITCH;
+    const bool wide = o.dtype == WFQ_F32;
 #pragma unroll 1
     for (int h = 0; h < CW; h += COLS) {
         __syncwarp();
@@ -391,8 +405,13 @@ __device__ __forceinline__ void finish_rows(const OutArgs &o, float *patch, int 
             }
         __syncwarp();
         const int k = k0 + h + 8 * piece;                         // first column of this lane's piece
+        if (o.residual) {
+            if (wide) ptx::copy_async_wait<0>();
+            else ptx::copy_async_wait<1>();                       // the next 32 columns may still be on their way
+        }
         if (o.vec && k + 8 <= o.Kz) {
             const int j = o.gated ? k / 2 : k;
+            const float *res = residual + (!wide && h % 64 ? 512 : 0) + 4 * lane;
             float b[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -400,7 +419,7 @@ __device__ __forceinline__ void finish_rows(const OutArgs &o, float *patch, int 
 #pragma unroll 1
             for (int q = 0; q < 32; q += ROWS) {
                 const long long r = row0 + q + r_in;
-                if (r >= o.R) continue;
+                if (r >= o.R) break;
                 float z[8];
                 const float4 *src = reinterpret_cast<const float4 *>(patch + (q + r_in) * PITCH + 8 * piece);
                 const int odd = r_in & 1;
@@ -413,11 +432,11 @@ __device__ __forceinline__ void finish_rows(const OutArgs &o, float *patch, int 
                     activate_all(y, o.act);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) y[i] *= z[2 * i + 1];
-                    if (o.residual) add_packed(y, load_packed<4>(o.residual, r * o.ldr + j, o.dtype), o.dtype);
+                    if (o.residual) add_residual(y, res + q / ROWS * 128, 512, o.dtype);
                     store_packed(o.y, r * o.ldy + j, y, o.dtype);
                 } else {
                     activate_all(z, o.act);
-                    if (o.residual) add_packed(z, load_packed<8>(o.residual, r * o.ldr + j, o.dtype), o.dtype);
+                    if (o.residual) add_residual(z, res + q / ROWS * 128, 512, o.dtype);
                     store_packed(o.y, r * o.ldy + j, z, o.dtype);
                 }
             }
@@ -430,6 +449,7 @@ __device__ __forceinline__ void finish_rows(const OutArgs &o, float *patch, int 
                     finish_pair(o, row0 + q + r_in, k + i, src[0], src[1]);
                 }
         }
+        if (o.residual) ask_residual<CW>(o, ptx::smem_u32(residual), lane, row0, k0, h + (wide ? 32 : 64));
     }
 }
 
@@ -494,13 +514,10 @@ __device__ __forceinline__ bool epilogue_tile(Shared *sh, const MmaArgs &a, cons
     Sums<CW, SWAP> sums;
     sums.zero();
     if constexpr (!SWAP) {
-        // the residual's lines on their way to L2 while the sums are formed (4096 x 128 -> 4096 fp32 66 -> 50 us; asking for
-        // them in registers ahead of their use costs the promotion more in spills than it gains here)
-        const long long r = row0 + quarter * 32 + lane;
-        if (a.out.residual && active && a.split == 1 && r < a.out.R) {
-            const int elem = a.out.dtype == WFQ_F32 ? 4 : 2, j0 = (col0 + ec.c0) >> a.out.gated, n = CW >> a.out.gated;
-            const char *line = static_cast<const char *>(a.out.residual) + (r * a.out.ldr + j0) * elem;
-            for (int i = 0; i < n && j0 + i < a.out.K; i += 128 / elem) ptx::prefetch_l2(line + i * elem);
+        if (a.out.residual && active && a.split == 1) {
+            const uint32_t buffer = ptx::smem_u32(ec.patch + 32 * PATCH_PITCH);
+            ask_residual<CW>(a.out, buffer, lane, row0 + quarter * 32, col0 + ec.c0, 0);
+            if (a.out.dtype != WFQ_F32) ask_residual<CW>(a.out, buffer, lane, row0 + quarter * 32, col0 + ec.c0, 32);
         }
     }
     bool ready = false;              // the slot was seen to be full ahead of its turn

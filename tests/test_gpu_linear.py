@@ -53,6 +53,14 @@ def test_epilogues(dtype, gated, act, shape):
     _case(7 if shape == 14004 else 35, 1024, 75, 128, dtype, act=act, bias=True, residual=True, gated=gated, shape=shape, codes=gated)
 
 
+@pytest.mark.parametrize("shape", [11064, 11128, 13128, 13256])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_residual_over_many_tiles(dtype, gated, shape):
+    """Several tiles per CTA, ragged in both directions, with rows of y and the residual that allow wide accesses."""
+    _case(1300, 160, 2056, 64, dtype, act="silu", bias=True, residual=True, gated=gated, shape=shape)
+
+
 @pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 8, 9, 16, 17, 31, 64, 65, 127, 128, 129, 500])
 @pytest.mark.parametrize("C,K,gs,dtype", [(640, 1280, 64, "f16"), (768, 320, 32, "bf16"), (1009, 77, 128, "f32")])
 def test_rows(rows, C, K, gs, dtype):
