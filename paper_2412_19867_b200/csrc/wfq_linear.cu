@@ -225,21 +225,25 @@ __device__ __forceinline__ void add_residual(float (&y)[N], const float *piece, 
 }
 // N (4 or 8) consecutive values of y, aligned to their size up to 16 bytes.
 template <int N>
-__device__ __forceinline__ void store_packed(void *p, long long i, const float (&y)[N], int dtype)
+__device__ __forceinline__ void store_packed(char *p, const float (&y)[N], int dtype)
 {
     if (dtype == WFQ_F32) {
-        float4 *q = reinterpret_cast<float4 *>(static_cast<float *>(p) + i);
+        float4 *q = reinterpret_cast<float4 *>(p);
 #pragma unroll
         for (int e = 0; e < N / 4; ++e) q[e] = make_float4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
         return;
     }
-    const int kind = dtype == WFQ_F16 ? 1 : 2;
     uint32_t w[N / 2];
+    if (dtype == WFQ_F16) {
 #pragma unroll
-    for (int e = 0; e < N / 2; ++e) w[e] = to_bits16x2(y[2 * e], y[2 * e + 1], kind);
-    uint16_t *q = static_cast<uint16_t *>(p) + i;
-    if constexpr (N == 8) *reinterpret_cast<uint4 *>(q) = make_uint4(w[0], w[1], w[2], w[3]);
-    else *reinterpret_cast<uint2 *>(q) = make_uint2(w[0], w[1]);
+        for (int e = 0; e < N / 2; ++e) *reinterpret_cast<__half2 *>(&w[e]) = __floats2half2_rn(y[2 * e], y[2 * e + 1]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N / 2; ++e)
+            *reinterpret_cast<__nv_bfloat162 *>(&w[e]) = __floats2bfloat162_rn(y[2 * e], y[2 * e + 1]);
+    }
+    if constexpr (N == 8) *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
 }
 
 template <int N>
@@ -390,6 +394,7 @@ __device__ __forceinline__ void finish_rows(const OutArgs &o, float *patch, int 
     const int piece = lane % PIECES, r_in = lane / PIECES;
     float *residual = patch + 32 * PATCH_PITCH;
     const bool wide = o.dtype == WFQ_F32;
+    const int elem = wide ? 4 : 2;
 #pragma unroll 1
     for (int h = 0; h < CW; h += COLS) {
         __syncwarp();
@@ -416,15 +421,18 @@ __device__ __forceinline__ void finish_rows(const OutArgs &o, float *patch, int 
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 b[i] = !o.bias ? 0.f : o.gated ? __ldg(o.bias + (i & 1 ? o.K : 0) + j + i / 2) : __ldg(o.bias + j + i);
+            const int odd = r_in & 1;
+            const float4 *src = reinterpret_cast<const float4 *>(patch + r_in * PITCH + 8 * piece);
+            float4 s0 = src[odd], s1 = src[odd ^ 1];
+            const int live = o.R - row0 - r_in;                   // steps q < live have a row
+            const long long first = (row0 + r_in) * o.ldy + j, step = ROWS * o.ldy;
+            char *to = static_cast<char *>(o.y) + first * elem;
 #pragma unroll 1
-            for (int q = 0; q < 32; q += ROWS) {
-                const long long r = row0 + q + r_in;
-                if (r >= o.R) break;
+            for (int q = 0; q < 32 && q < live; q += ROWS, to += step * elem) {
                 float z[8];
-                const float4 *src = reinterpret_cast<const float4 *>(patch + (q + r_in) * PITCH + 8 * piece);
-                const int odd = r_in & 1;
-                const float4 s0 = src[odd], s1 = src[odd ^ 1];
                 const float4 lo = odd ? s1 : s0, hi = odd ? s0 : s1;
+                src += ROWS * PITCH / 4;
+                if (q + ROWS < 32) { s0 = src[odd]; s1 = src[odd ^ 1]; }      // the next step's, on their way meanwhile
                 z[0] = lo.x + b[0]; z[1] = lo.y + b[1]; z[2] = lo.z + b[2]; z[3] = lo.w + b[3];
                 z[4] = hi.x + b[4]; z[5] = hi.y + b[5]; z[6] = hi.z + b[6]; z[7] = hi.w + b[7];
                 if (o.gated) {
@@ -433,11 +441,11 @@ __device__ __forceinline__ void finish_rows(const OutArgs &o, float *patch, int 
 #pragma unroll
                     for (int i = 0; i < 4; ++i) y[i] *= z[2 * i + 1];
                     if (o.residual) add_residual(y, res + q / ROWS * 128, 512, o.dtype);
-                    store_packed(o.y, r * o.ldy + j, y, o.dtype);
+                    store_packed(to, y, o.dtype);
                 } else {
                     activate_all(z, o.act);
                     if (o.residual) add_residual(z, res + q / ROWS * 128, 512, o.dtype);
-                    store_packed(o.y, r * o.ldy + j, z, o.dtype);
+                    store_packed(to, z, o.dtype);
                 }
             }
         } else {
@@ -852,6 +860,7 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             const int mt = t % a.MT, nt = t / a.MT;
             if (!epilogue_tile<BN, SWAP, PAIR>(sh, a, ctx, ec, mt * row_block + row_off, nt * BN, rg, slot, sphase)) break;
         }
+        if constexpr (!SWAP) ptx::copy_async_wait<0>();      // where a wait ran out, residuals may still be on their way
     }
 
     __syncwarp();
@@ -1287,7 +1296,7 @@ cudaError_t launch_dot(const wfq_linear &l, const void *x, long long ldx, const 
     return launch_dot_rows<__nv_bfloat16>(a, grid, smem, stream);
 }
 
-const Shape shape_for(wfq_linear &l, int rows)
+Shape shape_for(wfq_linear &l, int rows)
 {
     if (l.shape_rows != rows) {
         const Shape s = choose(l, rows);
@@ -1488,6 +1497,9 @@ wfq_status_t wfq_linear_prepare_weights(wfq_linear_t *l, const void *w_dev, long
     const wfq_status_t s = bind(l);
     if (s != WFQ_OK) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) return WFQ_ERR_CUDA;
+    if (cap != cudaStreamCaptureStatusNone && !l->status) return WFQ_ERR_INVALID_ARG;       // cudaMalloc ends a capture
     cudaError_t e;
     if (!l->Wq && (e = cudaMalloc(&l->Wq, (size_t)l->Kz * l->Cp)) != cudaSuccess) return to_status(e);
     if (!l->sW) {
@@ -1510,8 +1522,6 @@ wfq_status_t wfq_linear_prepare_weights(wfq_linear_t *l, const void *w_dev, long
     a.gs = l->gs; a.G = l->G;
     a.scale_pitch = l->Kp;
     a.half = l->gated ? l->K : 0;
-    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
-    if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) return WFQ_ERR_CUDA;
     if (cap != cudaStreamCaptureStatusNone) l->written_by_graph = true;
     l->fresh = true;
     if (launch_rows(a, dtype, st, false) != cudaSuccess) { l->prepared = false; return WFQ_ERR_CUDA; }
