@@ -385,7 +385,7 @@ wfq_status_t wfq_plan_destroy(wfq_plan_t *plan);
 /*
  * h = x + residual, rounded once to `dtype` (without a residual h = x);
  * u = fl32(h * gain[c]),  rstd = 1 / sqrt(mean(h^2) + eps), sums in fp32 (rows of values whose squares do not fit it,
- * above about 1e18, are not supported: their scales become 0 or NaN);
+ * above about 1e18, are not supported: their scales become 0 or NaN; nor, with eps 0, rows below about 1e-18);
  * codes = the quantizer's codes of u, scales = the quantizer's scales of u times rstd.
  * The factor rstd is common to a row and cancels in the codes, which therefore do not depend on its rounding.
  *   x_dev, residual_dev  device, `dtype`, [rows][C] with leading dimensions ldx, ldr; residual_dev may be NULL
@@ -438,16 +438,20 @@ wfq_status_t wfq_linear_set_workspace(wfq_linear_t *lin, void *dev_ptr, size_t b
 
 /*
  * Quantizes the weights w[K][C] ([2K][C] if gated), leading dimension ldw, into buffers that the layer owns (allocated
- * with cudaMalloc by the first call).  Asynchronous on `stream`; may be called again to replace them.
+ * with cudaMalloc by the first call, which is refused with WFQ_ERR_INVALID_ARG under stream capture).  Asynchronous on
+ * `stream`; may be called again to replace them.
  */
 wfq_status_t wfq_linear_prepare_weights(wfq_linear_t *lin, const void *w_dev, long long ldw, wfq_dtype_t dtype,
                                         void *stream);
 
 /*
  * y = the layer on x[rows][C] (quantized on the way), or on rows that are quantized already with the layer's C and group
- * size.  residual_dev may be NULL, or y_dev itself with the same leading dimension.  y does not overlap x or the codes.
+ * size.  residual_dev may be NULL, or y_dev itself with the same leading dimension, otherwise it does not overlap y; nor
+ * does y overlap x or the codes.
  * WFQ_ERR_NOT_PREPARED without weights or workspace, WFQ_ERR_INVALID_ARG for more rows than the workspace is for.  One
- * layer must not be used from two threads or two streams at the same time.
+ * layer must not be used from two threads at the same time, nor on two streams, or in two graphs that run at the same
+ * time: its calls share one workspace.  A graph keeps the addresses of the workspace, the weights and the bias that it was
+ * captured with; weights that are prepared again later are the ones that its next replay uses.
  */
 wfq_status_t wfq_linear_forward(wfq_linear_t *lin, const void *x_dev, long long ldx, int rows, const void *residual_dev,
                                 long long ldr, void *y_dev, long long ldy, void *stream);

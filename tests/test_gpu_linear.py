@@ -291,3 +291,22 @@ def test_weights_written_by_a_graph(rows):
         fresh.prepare(w)
         want = fresh.forward_codes(q)
         assert torch.equal(inside, want) and torch.equal(outside, want)
+
+
+def test_first_preparation_under_capture_is_refused():
+    """It allocates, which would end the capture: the call fails, the capture and the layer go on."""
+    x = torch.randn(5, 96, device="cuda")
+    w = torch.randn(40, 96, device="cuda")
+    layer = b.Linear(96, 40, 32, 8, "f32")
+    out = torch.zeros(8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(b.WfqError) as err:
+            layer.prepare(w)
+        out += 1
+    assert err.value.status == b.WFQ_ERR_INVALID_ARG
+    graph.replay()
+    assert out.tolist() == [1.0] * 8
+    layer.prepare(w)
+    assert torch.isfinite(layer.forward(x)).all()
+    layer.check_status()
