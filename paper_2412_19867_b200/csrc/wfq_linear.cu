@@ -15,10 +15,10 @@
 // With few tiles a cluster of up to eight CTAs shares one: each takes a range of the channels, the partial sums are
 // added in rank order through distributed shared memory, each CTA for a share of the columns.
 // What bounds it.  Short groups: the epilogue's arithmetic, a conversion and two products per group sum.  2048 x 8192 ->
-// 2048 in groups of 128 on pairs (one tile per pair of CTAs): 61 us, 1.1 POPS; a piece of 128 x 256 sums takes the eight
+// 2048 in groups of 128 on pairs (one tile per pair of CTAs): 60 us, 1.1 POPS; a piece of 128 x 256 sums takes the eight
 // epilogue warps 1200 cycles, of which the conversions are 300, one product 250, the loads 160, against 512 of its MMAs.
 // Long groups: the MMAs at the clock that the power limit leaves; 8192 x 4096 -> 8192 with one scale per row 178 us,
-// 3.1 POPS of the 4.6 that MMAs without loads reach.  Few rows: the weights' bytes; 24 x 4096 -> 32768 30 us, 4.5 TB/s,
+// 3.1 POPS of the 4.6 that MMAs without loads reach.  Few rows: the weights' bytes; 24 x 4096 -> 32768 31 us, 4.4 TB/s,
 // where 256 tiles on 148 SMs leave the second round half empty.
 // Every wait is bounded; on expiry the CTA records where, stops, drains and frees TMEM.
 #include <cuda_bf16.h>
