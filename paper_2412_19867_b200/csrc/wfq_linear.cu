@@ -933,9 +933,10 @@ linear_mma_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
 constexpr int DOT_THREADS = 256, DOT_WARPS = DOT_THREADS / 32, DOT_COLS = 4, DOT_AHEAD = 2;
 constexpr int DOT_MAX_ROWS = 8;
 constexpr int DOT_SMEM_MAX = 96 * 1024;
-// Values that a CTA quantizes for itself: as many as its registers keep.  Beyond, reading them twice in every CTA takes
-// longer than a launch (4 rows of 8192 channels: 46 us).
-constexpr int DOT_KEEP = 4;
+// Values that a CTA quantizes for itself: what its registers keep without taking them from the products.  With twice as many
+// 2 x 4096 -> 4096 takes 10.7 us and 1 x 4096 8.5 us, against 8.7 and 8.0 us (the first through the row quantizer); every
+// CTA reading 4 rows of 8192 twice takes 46 us.  Where the host is the bound the quantizer's launch costs 2 us.
+constexpr int DOT_KEEP = 2;
 constexpr int DOT_QUANTIZE_MAX = 8 * DOT_THREADS * DOT_KEEP;
 
 struct DotArgs {
