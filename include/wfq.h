@@ -378,8 +378,9 @@ wfq_status_t wfq_plan_destroy(wfq_plan_t *plan);
  *
  * Supported: 1 <= C <= 131072; rows >= 0 (0: nothing is done); leading dimensions (elements from row to row) of at least
  * the row's width, without alignment beyond the element's.  codes must be 32-byte aligned, scales 16-byte.
- * Rows with 16-byte aligned starts and a C that is a multiple of 8 are read and written in wider pieces; the results are
- * the same.  All calls are asynchronous, allocate nothing unless stated, and may be captured into a graph.
+ * Rows with 16-byte aligned starts and a C that is a multiple of 8 are read and written in wider pieces, and those with a C
+ * that is a multiple of 4 and starts aligned to four elements in pieces of four; the results are the same.  All calls are
+ * asynchronous, allocate nothing unless stated, and may be captured into a graph.
  */
 
 /*

@@ -11,6 +11,7 @@
 #include <cuda_fp16.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "wfq_ptx.cuh"
 #include "wfq_rows.h"
@@ -33,18 +34,18 @@ template <> struct Elem<__nv_bfloat16> {
     static __device__ __forceinline__ __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
 };
 
-// Eight consecutive elements, 16-byte aligned.
-template <typename T> __device__ __forceinline__ void store8(T *p, const float (&v)[8])
+// N (8 or 4) consecutive elements, aligned to their size up to 16 bytes.
+template <int N, typename T> __device__ __forceinline__ void store_wide(T *p, const float (&v)[N])
 {
     if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
-        *reinterpret_cast<float4 *>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+#pragma unroll
+        for (int i = 0; i < N; i += 4) *reinterpret_cast<float4 *>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
     } else {
-        uint4 a;
+        typename std::conditional<N == 8, uint4, uint2>::type a;
         T *e = reinterpret_cast<T *>(&a);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = Elem<T>::put(v[i]);
-        *reinterpret_cast<uint4 *>(p) = a;
+        for (int i = 0; i < N; ++i) e[i] = Elem<T>::put(v[i]);
+        *reinterpret_cast<decltype(a) *>(p) = a;
     }
 }
 
@@ -136,44 +137,49 @@ __global__ void __launch_bounds__(256) rows_any_kernel(RowsArgs a)
     }
 }
 
-// a += b for eight elements, each sum rounded once.  A 16-bit sum rounded from 32 bits is the same: where 32 bits do not
+// a += b for N elements, each sum rounded once.  A 16-bit sum rounded from 32 bits is the same: where 32 bits do not
 // hold it exactly the smaller term is less than a quarter of a step of the larger.
-__device__ __forceinline__ void add_words(float *a, const float *b)
+template <int N> __device__ __forceinline__ void add_words(float *a, const float *b)
 {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) a[i] = __fadd_rn(a[i], b[i]);
+    for (int i = 0; i < N; ++i) a[i] = __fadd_rn(a[i], b[i]);
 }
-__device__ __forceinline__ void add_words(__half *a, const __half *b)
+template <int N> __device__ __forceinline__ void add_words(__half *a, const __half *b)
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < N / 2; ++i)
         reinterpret_cast<__half2 *>(a)[i] = __hadd2(reinterpret_cast<__half2 *>(a)[i], reinterpret_cast<const __half2 *>(b)[i]);
 }
-__device__ __forceinline__ void add_words(__nv_bfloat16 *a, const __nv_bfloat16 *b)
+template <int N> __device__ __forceinline__ void add_words(__nv_bfloat16 *a, const __nv_bfloat16 *b)
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < N / 2; ++i)
         reinterpret_cast<__nv_bfloat162 *>(a)[i] =
             __hadd2(reinterpret_cast<__nv_bfloat162 *>(a)[i], reinterpret_cast<const __nv_bfloat162 *>(b)[i]);
 }
 
-// VEC consecutive elements as they lie in memory (VEC 8: 16-byte aligned).
+// VEC (8 or 4) consecutive elements as they lie in memory, aligned to their size up to 16 bytes.
 template <typename T, int VEC> struct Raw {
-    uint4 q[sizeof(T) / 2];
+    using Word = typename std::conditional<sizeof(T) * VEC == 8, uint2, uint4>::type;
+    static constexpr int N = (int)(sizeof(T) * VEC / sizeof(Word));
+    Word q[N];
     __device__ __forceinline__ void load(const T *p)
     {
-        const uint4 *src = reinterpret_cast<const uint4 *>(p);
+        const Word *src = reinterpret_cast<const Word *>(p);
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) q[i] = src[i];
+        for (int i = 0; i < N; ++i) q[i] = src[i];
     }
     __device__ __forceinline__ void put(T *p) const
     {
-        uint4 *dst = reinterpret_cast<uint4 *>(p);
+        Word *dst = reinterpret_cast<Word *>(p);
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) dst[i] = q[i];
+        for (int i = 0; i < N; ++i) dst[i] = q[i];
     }
     __device__ __forceinline__ float get(int e) const { return Elem<T>::get(reinterpret_cast<const T *>(q)[e]); }
-    __device__ __forceinline__ void add(const Raw &o) { add_words(reinterpret_cast<T *>(q), reinterpret_cast<const T *>(o.q)); }
+    __device__ __forceinline__ void add(const Raw &o)
+    {
+        add_words<VEC>(reinterpret_cast<T *>(q), reinterpret_cast<const T *>(o.q));
+    }
 };
 template <typename T> struct Raw<T, 1> {
     T v;
@@ -188,7 +194,7 @@ template <typename T> struct Raw<T, 1> {
 };
 template <int VEC, typename T> __device__ __forceinline__ void store(T *p, const float (&v)[VEC])
 {
-    if constexpr (VEC == 8) store8(p, v);
+    if constexpr (VEC > 1) store_wide<VEC>(p, v);
     else *p = Elem<T>::put(v[0]);
 }
 
@@ -200,7 +206,8 @@ template <int VEC, typename T> __device__ __forceinline__ void store(T *p, const
 // 16384 x 4096 bf16 with a residual 86 us, 5.5 TB/s (with 80 registers, three CTAs of 256 threads per SM, 100 us; without a
 // residual three are better, 16384 x 1280 23 against 34 us); 8192 x 4096 bf16 quantized alone 24 us, 4.2 TB/s.
 template <typename T, bool NORM, bool RES, int VEC, int NV, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? (RES && VEC == 8 ? 2 : 3) : 1) rows_kernel(RowsArgs a, int tpr, int lanes, int direct)
+__global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? (RES && VEC > 1 ? 2 : 3) : 1)
+rows_kernel(RowsArgs a, int tpr, int lanes, int direct)
 {
     extern __shared__ int group_max[];        // [2][rows of the CTA][G] where groups are joined, alternately
     __shared__ float warp_sum[2][32];
@@ -341,9 +348,14 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 && NV * VEC <= 16 ? (R
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) w[e] = code_bits(u[i][e], inv);
                     uint32_t lo = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
-                    uint32_t hi = __byte_perm(__byte_perm(w[4], w[5], 0x0040), __byte_perm(w[6], w[7], 0x0040), 0x5410);
-                    if (!(inv > 0.f)) lo = hi = 0;
-                    *reinterpret_cast<uint2 *>(codes + v * 8) = make_uint2(lo, hi);
+                    if (!(inv > 0.f)) lo = 0;
+                    if constexpr (VEC == 8) {
+                        uint32_t hi = __byte_perm(__byte_perm(w[4], w[5], 0x0040), __byte_perm(w[6], w[7], 0x0040), 0x5410);
+                        if (!(inv > 0.f)) hi = 0;
+                        *reinterpret_cast<uint2 *>(codes + v * 8) = make_uint2(lo, hi);
+                    } else {
+                        *reinterpret_cast<uint32_t *>(codes + v * 4) = lo;
+                    }
                 }
             }
         }
@@ -387,6 +399,7 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const int8_t *__restric
                 const int c = c0 + i * tpr * VEC;
                 if (c < C) {
                     if constexpr (VEC == 8) q[i] = __ldg(reinterpret_cast<const uint2 *>(codes + row * Cp + c));
+                    else if constexpr (VEC == 4) q[i].x = __ldg(reinterpret_cast<const uint32_t *>(codes + row * Cp + c));
                     else q[i].x = (uint32_t)(uint8_t)__ldg(codes + row * Cp + c);
                     s[i] = __ldg(scales + (size_t)(c / by_gs) * scale_pitch + row);
                 }
@@ -473,28 +486,35 @@ cudaError_t launch_rows_size(const RowsArgs &a, int tpr, cudaStream_t stream, bo
                       : launch_rows_mode<T, VEC, NV, 1024>(a, tpr, stream, pdl);
 }
 
-bool aligned16(const void *p, long long ld, size_t elem)
+bool aligned(const void *p, long long ld, size_t elem, size_t bytes)
 {
-    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (size_t)ld * elem % 16 == 0;
+    return reinterpret_cast<uintptr_t>(p) % bytes == 0 && (size_t)ld * elem % bytes == 0;
 }
 
 template <typename T>
 cudaError_t launch_rows_t(const RowsArgs &a, cudaStream_t stream, bool pdl)
 {
     const size_t e = sizeof(T);
-    const bool wide = a.C % 8 == 0 && aligned16(a.x, a.ldx, e) && (!a.residual || aligned16(a.residual, a.ldr, e)) &&
-                      (!a.h || aligned16(a.h, a.ldh, e)) && (!a.gain || aligned16(a.gain, 0, 4));
+    auto pieces = [&](int n) {       // do all rows consist of pieces of n elements, aligned to their size up to 16 bytes?
+        const size_t bytes = n * e < 16 ? n * e : 16;
+        return a.C % n == 0 && aligned(a.x, a.ldx, e, bytes) && (!a.residual || aligned(a.residual, a.ldr, e, bytes)) &&
+               (!a.h || aligned(a.h, a.ldh, e, bytes));
+    };
+    // pieces of four: 9424 x 1500 fp16 norm with residual 25.6 us, element by element 57; 2000 x 4100 fp32 36 against 95
+    const int vec = pieces(8) ? 8 : pieces(4) ? 4 : 1;
     // Elements per thread: 8 where there are few rows (latency) or the elements are single or 32-bit loads, else 16; 32 for
     // rows that would not fit a CTA otherwise.
-    const int want = !wide || e == 4 || a.rows < 592 ? 8 : 16;
+    const int want = vec == 1 || e == 4 || a.rows < 592 ? 8 : 16;
     for (int per : {8, 16, 32}) {
         const int tpr = ((a.Cp + per - 1) / per + 31) / 32 * 32;
         if (tpr > 1024 || per < want || a.G > 2048) continue;
-        if (wide)
+        if (vec == 8)
             return per == 8 ? launch_rows_size<T, 8, 1>(a, tpr, stream, pdl)
                             : per == 16 ? launch_rows_size<T, 8, 2>(a, tpr, stream, pdl)
                                         : launch_rows_size<T, 8, 4>(a, tpr, stream, pdl);
-        if (per == 8) return launch_rows_size<T, 1, 8>(a, tpr, stream, pdl);
+        if (vec == 4 && per <= 16)
+            return per == 8 ? launch_rows_size<T, 4, 2>(a, tpr, stream, pdl) : launch_rows_size<T, 4, 4>(a, tpr, stream, pdl);
+        if (vec == 1 && per == 8) return launch_rows_size<T, 1, 8>(a, tpr, stream, pdl);
     }
     const int grid = a.rows < (1 << 20) ? a.rows : 1 << 20;
     const size_t smem = (size_t)a.G * sizeof(int);
@@ -506,14 +526,14 @@ template <typename T>
 cudaError_t launch_dequantize(const int8_t *codes, const float *scales, int rows, int C, int gs, void *v, long long ldv,
                               cudaStream_t stream)
 {
-    const bool wide = C % 8 == 0 && aligned16(v, ldv, sizeof(T));
-    const int n = wide ? C / 8 : C, tpr = n >= 256 ? 256 : (n + 31) / 32 * 32, per_cta = 256 / tpr;
+    constexpr size_t e = sizeof(T);
+    const int vec = C % 8 == 0 && aligned(v, ldv, e, 16) ? 8 : C % 4 == 0 && aligned(v, ldv, e, 4 * e) ? 4 : 1;
+    const int n = C / vec, tpr = n >= 256 ? 256 : (n + 31) / 32 * 32, per_cta = 256 / tpr;
     const long long ctas = (rows + (long long)per_cta - 1) / per_cta, pitch = (rows + 127LL) / 128 * 128;
     const dim3 grid((unsigned)(ctas < (1 << 20) ? ctas : 1 << 20));
-    return wide ? launch(dequantize_kernel<T, 8>, grid, 256, 0, stream, true, codes, scales, rows, C, row_pitch_codes(C),
-                         FastDiv(gs), pitch, static_cast<T *>(v), ldv, tpr)
-                : launch(dequantize_kernel<T, 1>, grid, 256, 0, stream, true, codes, scales, rows, C, row_pitch_codes(C),
-                         FastDiv(gs), pitch, static_cast<T *>(v), ldv, tpr);
+    auto kernel = vec == 8 ? dequantize_kernel<T, 8> : vec == 4 ? dequantize_kernel<T, 4> : dequantize_kernel<T, 1>;
+    return launch(kernel, grid, 256, 0, stream, true, codes, scales, rows, C, row_pitch_codes(C), FastDiv(gs), pitch,
+                  static_cast<T *>(v), ldv, tpr);
 }
 
 bool known(wfq_dtype_t t) { return t == WFQ_F32 || t == WFQ_F16 || t == WFQ_BF16; }

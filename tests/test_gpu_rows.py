@@ -191,3 +191,36 @@ def test_other_stream_and_graph():
     want, want_h = b.rms_norm_quantize(x, gain, residual=res)
     assert torch.equal(q.codes, want.codes) and torch.equal(q.scales[:, :50], want.scales[:, :50])
     assert torch.equal(h, want_h) and torch.equal(v, b.dequantize_rows(want, "bf16"))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,C,gs", [(1, 4, 32), (3, 36, 32), (700, 100, 32), (601, 1500, 128), (5, 772, 0), (40, 4100, 160),
+                                       (3, 12300, 64), (2, 20004, 256), (2, 131068, 0)])
+def test_rows_in_pieces_of_four(rows, C, gs, dtype):
+    """C a multiple of 4, not of 8: as they are, and inside wider rows that begin four elements in."""
+    gain = torch.linspace(0.5, 2, C + 1, device="cuda")[1:]
+    for ld, offset in ((C, 0), (C + 8, 4), (C + 4, 0)):
+        x = _rows(1, rows * ld + offset, dtype, C)[0][offset:].as_strided((rows, C), (ld, 1))
+        res = _rows(rows, C, dtype, 1)
+        q = b.quantize_rows(x, gs)
+        _check(q, *ref.quantize(x, gs), 0.0)
+        h, codes, scales = ref.rms_norm_quantize(x, res, gain, 1e-5, gs)
+        out = torch.full((rows * ld + offset,), 7.0, dtype=dtype, device="cuda")
+        view = out[offset:].as_strided((rows, C), (ld, 1))
+        qn, got = b.rms_norm_quantize(x, gain, 1e-5, gs, residual=res, out=view)
+        _check(qn, codes, scales, ref.norm_scale_tolerance(C))
+        assert torch.equal(got.cpu(), h)
+        _, codes, scales = ref.rms_norm_quantize(x, None, gain, 1e-5, gs)
+        _check(b.rms_norm_quantize(x, gain, 1e-5, gs)[0], codes, scales, ref.norm_scale_tolerance(C))
+        name = {torch.float32: "f32", torch.float16: "f16", torch.bfloat16: "bf16"}[dtype]
+        values = torch.full((rows * ld + offset,), 7.0, dtype=dtype, device="cuda")
+        to = values[offset:].as_strided((rows, C), (ld, 1))
+        b.wfq_dequantize_rows(q.codes.data_ptr(), q.scales.data_ptr(), rows, C, gs, b._DTYPES[name], to.data_ptr(), ld,
+                              torch.cuda.current_stream().cuda_stream)
+        assert torch.equal(to, b.dequantize_rows(q, name))
+        want = q.codes[:, :C].double() * ref.spread(q.scales[:, :rows].T.double().cpu(), C, gs).cuda()
+        half = torch.finfo(dtype).eps / 2
+        assert ((to.double() - want).abs() <= half * want.abs() * (1 + 2.0 ** -12) + 2.0 ** -25).all()
+        kept = torch.ones_like(out, dtype=torch.bool)
+        kept[offset:].as_strided((rows, C), (ld, 1)).fill_(False)
+        assert (out[kept] == 7.0).all() and (values[kept] == 7.0).all()
