@@ -38,6 +38,7 @@ struct wfq_linear {
     const float *bias = nullptr;
     int act = 0;
     int device = -1, sm_count = 0;
+    int clusters[4] = {0, 0, 0, 0};            // of 1, 2, 4 and 8 CTAs that run at once
     int8_t *Wq = nullptr;                      // [Kz][Cp]
     CUtensorMap tmap_w[2];                     // Wq in boxes of 64 and of 128 rows x 128 channels
     bool tmap_w_ok[2] = {false, false};
@@ -1158,13 +1159,18 @@ bool known_shape(const Shape &s)
     return s.orient == 3 && s.split == 1 && (s.bn == 128 || s.bn == 256);
 }
 
-// Microseconds of a tile, from sweeps over the shapes below (rows 1 to 8192, groups of 32 to 128 and whole rows): a stage
-// of 128 channels takes its copies and MMAs or the promotion of its chunks, whichever is longer; then the results' way out.
+// Microseconds of a tile: a stage of 128 channels takes its copies and MMAs or the promotion of its chunks, whichever is
+// longer; then the results' way out, or, where CTAs share the channels, the sum of their parts (kSharedOut whatever the
+// shape).  Fitted to the times of every shape on 170 random sizes (32 to 8192 rows, 32 to 8192 channels, 128 to 32768
+// columns of z, groups of 32 to whole rows, all types); on 148 others the chosen shape takes 4 % longer than the best of
+// them in the mean, 13 % or less on nine out of ten and 39 % at worst.
 struct TileTime { double stage, chunk, piece, out; };
+constexpr double kSharedOut = 3.9;
 TileTime tile_time(const Shape &s)
 {
-    if (s.orient == 2) return s.bn == 16 ? TileTime{.27, .2, .03, .3} : s.bn == 32 ? TileTime{.29, .2, .06, .4} : TileTime{.34, .2, .2, .8};
-    return s.bn == 64 ? TileTime{.25, .33, .05, 1.2} : s.bn == 128 ? TileTime{.26, .2, .3, 1.8} : TileTime{.37, .25, .62, 3.};
+    if (s.orient == 2) return s.bn == 16 ? TileTime{.31, .09, .02, 2.} : s.bn == 32 ? TileTime{.25, .18, .03, 6.2} : TileTime{.16, .23, .11, 7.2};
+    if (s.orient == 3) return s.bn == 128 ? TileTime{.26, .34, .32, 4.3} : TileTime{.4, .33, .71, 8.7};
+    return s.bn == 64 ? TileTime{.21, .2, .15, 2.2} : TileTime{.35, .25, .45, 3.5};
 }
 
 Shape choose(const wfq_linear &l, int rows)
@@ -1175,9 +1181,10 @@ Shape choose(const wfq_linear &l, int rows)
     const int KB = (l.Cp / 32 + 3) / 4;
     Shape best{1, 64, 1};
     double best_cost = 1e300;
-    if (dot) {       // bytes at a rate that falls with the rows' arithmetic, less the tensor kernels' longer way in and out
+    if (dot) {       // bytes at a rate that falls with the rows' arithmetic (4096 -> 4096: 1 row 6.3 us, 4 rows 8.1; shared
+                     // tensor-core tiles 6.9 and 7.1)
         best = Shape{4, 4, 1};
-        best_cost = (double)l.Kz * l.Cp / (rows <= 2 ? 5.0e6 : rows <= 4 ? 3.6e6 : 2.2e6) - 2.2;
+        best_cost = (double)l.Kz * l.Cp / (rows <= 2 ? 4.2e6 : rows <= 4 ? 2.8e6 : 2.0e6) + .7;
     }
     for (int orient = 1; orient <= 3; ++orient)
         for (int bn : {256, 128, 64, 32, 16})
@@ -1187,7 +1194,10 @@ Shape choose(const wfq_linear &l, int rows)
                 const int lanes = orient == 3 ? 2 * BM : BM, per_tile = orient == 3 ? 2 : split;
                 const int r = orient == 2 ? l.Kz : rows, c = orient == 2 ? rows : l.Kz;
                 const double tiles = (double)((r + lanes - 1) / lanes) * ((c + bn - 1) / bn);
-                if (split > 1 && (tiles * split > l.sm_count || KB < 2 * split)) continue;
+                // Clusters beyond those that run at once would take a second round: 16 of 8 CTAs do not fit the processor
+                // clusters of 148 SMs, 8192 -> 2048 12.9 us instead of 7.2 us for the 14 of 8192 -> 1792.
+                const int log2_split = split == 8 ? 3 : split / 2;
+                if (split > 1 && (tiles > l.clusters[log2_split] || KB < 2 * split)) continue;
                 const TileTime t = tile_time(sp);
                 const int pieces = 512 / bn < 16 ? 512 / bn : 16, cg_max = pieces / 2 < 4 ? pieces / 2 : 4;
                 const int cg = BK % l.gs != 0 ? 1 : BK / l.gs < cg_max ? BK / l.gs : cg_max;
@@ -1195,7 +1205,7 @@ Shape choose(const wfq_linear &l, int rows)
                 if (stage < t.stage) stage = t.stage;
                 const int at_once = l.sm_count / per_tile;
                 const double waves = (double)(long long)((tiles + at_once - 1) / at_once);
-                const double cost = waves * ((KB + split - 1) / split * stage + t.out) + (split > 1 ? .8 : 0.);
+                const double cost = waves * ((KB + split - 1) / split * stage + (split > 1 ? kSharedOut : t.out));
                 if (cost < best_cost) { best_cost = cost; best = sp; }
             }
     return best;
@@ -1367,6 +1377,26 @@ wfq_status_t to_status(cudaError_t e)
     return e == cudaSuccess ? WFQ_OK : e == cudaErrorMemoryAllocation ? WFQ_ERR_ALLOC : WFQ_ERR_CUDA;
 }
 
+// How many clusters of 1 << i CTAs of the tensor-core kernels (one CTA per SM, whatever the shape) run at once.
+cudaError_t count_clusters(int (&clusters)[4])
+{
+    for (int i = 1; i < 4; ++i) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(1u << i);
+        cfg.blockDim = dim3(THREADS);
+        cfg.dynamicSmemBytes = Cfg<16, true, false>::SMEM_BYTES;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 1u << i;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        const cudaError_t e = cudaOccupancyMaxActiveClusters(&clusters[i], linear_mma_kernel<16, true, false>, &cfg);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
 // Binds the layer to the current device the first time, refuses another one later.
 wfq_status_t bind(wfq_linear *l)
 {
@@ -1386,6 +1416,7 @@ wfq_status_t bind(wfq_linear *l)
     if (e == cudaSuccess) e = setup_dot<float>();
     if (e == cudaSuccess) e = setup_dot<__half>();
     if (e == cudaSuccess) e = setup_dot<__nv_bfloat16>();
+    if (e == cudaSuccess) e = count_clusters(l->clusters);
     if (e != cudaSuccess) return WFQ_ERR_CUDA;
     l->device = dev;
     l->sm_count = sms;
