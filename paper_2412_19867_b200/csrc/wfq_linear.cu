@@ -1200,7 +1200,7 @@ Shape choose(const wfq_linear &l, int rows)
                 if (split > 1 && (tiles > l.clusters[log2_split] || KB < 2 * split)) continue;
                 const TileTime t = tile_time(sp);
                 const int pieces = 512 / bn < 16 ? 512 / bn : 16, cg_max = pieces / 2 < 4 ? pieces / 2 : 4;
-                const int cg = BK % l.gs != 0 ? 1 : BK / l.gs < cg_max ? BK / l.gs : cg_max;
+                const int cg = BK % l.gs != 0 || l.G == 1 ? 1 : BK / l.gs < cg_max ? BK / l.gs : cg_max;
                 double stage = 128.0 / l.gs / cg * (t.chunk + t.piece * cg);
                 if (stage < t.stage) stage = t.stage;
                 const int at_once = l.sm_count / per_tile;
@@ -1229,8 +1229,8 @@ cudaError_t setup_variant()
 template <int BN, bool SWAP, bool PAIR>
 cudaError_t launch_variant(wfq_linear &l, MmaArgs &a, int grid, const int8_t *xq, int rows, cudaStream_t stream)
 {
-    a.cg = 1;
-    if (BK % l.gs == 0) a.cg = BK / l.gs < Cfg<BN, SWAP, PAIR>::CG_MAX ? BK / l.gs : Cfg<BN, SWAP, PAIR>::CG_MAX;
+    a.cg = 1;                    // also where one group is all there is, however short: the MMA loop takes it as whole stages
+    if (BK % l.gs == 0 && l.G > 1) a.cg = BK / l.gs < Cfg<BN, SWAP, PAIR>::CG_MAX ? BK / l.gs : Cfg<BN, SWAP, PAIR>::CG_MAX;
     a.slots = Cfg<BN, SWAP, PAIR>::PIECES / a.cg;
     constexpr int w_rows = SWAP ? BM : Cfg<BN, SWAP, PAIR>::B_ROWS;
     constexpr int w_map = w_rows == 128 ? 1 : 0;

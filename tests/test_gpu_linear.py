@@ -310,3 +310,10 @@ def test_first_preparation_under_capture_is_refused():
     layer.prepare(w)
     assert torch.isfinite(layer.forward(x)).all()
     layer.check_status()
+
+
+@pytest.mark.parametrize("shape", [s for s in SHAPES if s // 10000 == 1 and s // 1000 % 10 != 4])
+@pytest.mark.parametrize("C,gs", [(32, 0), (64, 0), (64, 256), (64, 32), (96, 0), (128, 64), (160, 96), (224, 32)])
+def test_few_channels_over_many_tiles(C, gs, shape):
+    """Several tiles per CTA, each of one or two stages: every slot of tensor memory is used."""
+    _case(1500, C, 4100, gs, "bf16", shape=shape, codes=True, residual=True)
