@@ -150,11 +150,18 @@ __device__ __forceinline__ Range range_of(const MmaArgs &a, int rank)
     return r;
 }
 
+// NaN stays NaN (fmaxf would make it 0): what comes of a group with an infinity or a NaN in it is NaN.
+__device__ __forceinline__ float relu(float t)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(t));
+    return r;
+}
 __device__ __forceinline__ float gelu(float t) { return 0.5f * t * (1.f + erff(t * 0.70710678118654752f)); }
 __device__ __forceinline__ float activate(float t, int act)
 {
     switch (act) {
-        case WFQ_ACT_RELU: return fmaxf(t, 0.f);
+        case WFQ_ACT_RELU: return relu(t);
         case WFQ_ACT_SILU: return silu(t);
         case WFQ_ACT_GELU: return gelu(t);
         default: return t;
@@ -252,7 +259,7 @@ __device__ __forceinline__ void activate_all(float (&z)[N], int act)
 {
     if (act == WFQ_ACT_RELU) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) z[i] = fmaxf(z[i], 0.f);
+        for (int i = 0; i < N; ++i) z[i] = relu(z[i]);
     } else if (act == WFQ_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < N; ++i) z[i] = silu(z[i]);
