@@ -450,9 +450,11 @@ wfq_status_t wfq_linear_prepare_weights(wfq_linear_t *lin, const void *w_dev, lo
  * size.  residual_dev may be NULL, or y_dev itself with the same leading dimension, otherwise it does not overlap y; nor
  * does y overlap x or the codes.
  * WFQ_ERR_NOT_PREPARED without weights or workspace, WFQ_ERR_INVALID_ARG for more rows than the workspace is for.  One
- * layer must not be used from two threads at the same time, nor on two streams, or in two graphs that run at the same
- * time: its calls share one workspace.  A graph keeps the addresses of the workspace, the weights and the bias that it was
- * captured with; weights that are prepared again later are the ones that its next replay uses.
+ * layer must not be used from two threads at the same time.  wfq_linear_forward must not run on two streams, or in two
+ * graphs, at the same time either: its calls share one workspace.  wfq_linear_forward_codes uses none of it and may.  The
+ * caller orders products behind the preparation of their weights where they are on another stream, and the preparation of
+ * new weights behind products that still use the old ones.  A graph keeps the addresses of the workspace, the weights and
+ * the bias that it was captured with; weights that are prepared again later are the ones that its next replay uses.
  */
 wfq_status_t wfq_linear_forward(wfq_linear_t *lin, const void *x_dev, long long ldx, int rows, const void *residual_dev,
                                 long long ldr, void *y_dev, long long ldy, void *stream);

@@ -12,7 +12,7 @@ SOURCES = ["wfq_api.cu", "wfq_filter_prep.cu", "wfq_input_transform.cu", "wfq_in
            "wfq_input_transform_tcn.cu", "wfq_gemm.cu", "wfq_output_transform.cu", "wfq_full_quant.cu",
            "wfq_rows.cu", "wfq_linear.cu"]
 HEADERS = ["wfq_internal.h", "wfq_ptx.cuh", "wfq_quant.cuh", "wfq_int_quant.cuh", "wfq_strip.cuh",
-           "wfq_output_store.cuh", "wfq_rows.h"]
+           "wfq_output_store.cuh", "wfq_rows.h", "wfq_weight_order.h"]
 
 
 def _nvcc():

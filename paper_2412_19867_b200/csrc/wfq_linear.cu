@@ -30,6 +30,7 @@
 #include "wfq_output_store.cuh"
 #include "wfq_ptx.cuh"
 #include "wfq_rows.h"
+#include "wfq_weight_order.h"
 
 struct wfq_linear {
     int C = 0, K = 0, gs = 0, gated = 0;
@@ -45,8 +46,7 @@ struct wfq_linear {
     float *sW = nullptr;                       // [G][Kp], zero behind Kz
     int *status = nullptr;                     // int32[4]
     bool prepared = false;
-    bool fresh = false;                        // weights were written since the last product that waited for them
-    bool written_by_graph = false;             // a captured call writes them
+    wfq::WeightOrder order;                    // may a product fetch weights early?
     int8_t *xq = nullptr;                      // workspace: codes of up to max_rows rows
     float *sx = nullptr;
     int max_rows = 0;
@@ -1470,8 +1470,8 @@ wfq_status_t run(wfq_linear *l, const void *x, long long ldx, int8_t *xq, float 
     o.ldr = ldr; o.ldy = ldy;
     o.K = l->K; o.Kz = l->Kz; o.R = rows;
     o.act = l->act; o.gated = l->gated; o.dtype = (int)l->out_dtype;
-    const size_t e = elem_bytes(l->out_dtype);
-    o.vec = !misaligned(y, 16) && ldy * e % 16 == 0 && (!residual || (!misaligned(residual, 16) && ldr * e % 16 == 0));
+    const size_t elem = elem_bytes(l->out_dtype);
+    o.vec = !misaligned(y, 16) && ldy * elem % 16 == 0 && (!residual || (!misaligned(residual, 16) && ldr * elem % 16 == 0));
 
     const bool dot = shape_for(*l, rows).orient == 4;
     const bool quantize = x && !(dot && (long long)rows * l->Cp <= DOT_QUANTIZE_MAX);
@@ -1485,17 +1485,15 @@ wfq_status_t run(wfq_linear *l, const void *x, long long ldx, int8_t *xq, float 
         if (launch_rows(a, l->in_dtype, st, true) != cudaSuccess) return WFQ_ERR_CUDA;
     }
     // The product's launch may begin before the kernel in front of it has ended, and may fetch weights then if that cannot
-    // be the one that writes them: the row quantizer lets it begin only after its own wait for what was in front of it; and
-    // weights that were written since the last product are waited for.  Under capture the launch is only recorded, and the
-    // weights stay fresh; where a graph writes them, its replays do so unseen.
-    const bool early = quantize || !(l->fresh || l->written_by_graph);
-    if (l->fresh) {
-        cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
-        if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) return WFQ_ERR_CUDA;
-        if (cap == cudaStreamCaptureStatusNone) l->fresh = false;
-    }
-    if (dot) return to_status(launch_dot(*l, quantize ? nullptr : x, ldx, xq, sx, rows, o, st, early));
-    return to_status(launch_product(*l, xq, sx, rows, o, st));
+    // be the one that writes them: the row quantizer lets it begin only after its own wait for what was in front of it, and
+    // otherwise wfq_weight_order.h says.
+    const bool settled = l->order.settled(st), first = l->order.pending() && !settled;
+    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+    if (first && cudaStreamIsCapturing(st, &cap) != cudaSuccess) return WFQ_ERR_CUDA;
+    const cudaError_t e = dot ? launch_dot(*l, quantize ? nullptr : x, ldx, xq, sx, rows, o, st, quantize || settled)
+                              : launch_product(*l, xq, sx, rows, o, st);
+    if (e == cudaSuccess && first) l->order.waited(st, cap != cudaStreamCaptureStatusNone);
+    return to_status(e);
 }
 
 }  // namespace
@@ -1597,8 +1595,7 @@ wfq_status_t wfq_linear_prepare_weights(wfq_linear_t *l, const void *w_dev, long
     a.gs = l->gs; a.G = l->G;
     a.scale_pitch = l->Kp;
     a.half = l->gated ? l->K : 0;
-    if (cap != cudaStreamCaptureStatusNone) l->written_by_graph = true;
-    l->fresh = true;
+    l->order.written(st, cap != cudaStreamCaptureStatusNone);
     if (launch_rows(a, dtype, st, false) != cudaSuccess) { l->prepared = false; return WFQ_ERR_CUDA; }
     l->prepared = true;
     return WFQ_OK;
