@@ -264,8 +264,16 @@ def wfq_plan_destroy(plan):
     _check(load().wfq_plan_destroy(plan), "wfq_plan_destroy")
 
 
+def _sizes(*sizes):
+    """Refuses sizes that ctypes would cut to their low 32 bits."""
+    for n in sizes:
+        if not -2 ** 31 <= n < 2 ** 31:
+            raise WfqError(WFQ_ERR_UNSUPPORTED, f"size {n}")
+
+
 def wfq_rms_norm_quantize(x_dev, ldx, residual_dev, ldr, gain_dev, eps, dtype, rows, C, group_size, h_dev, ldh,
                           codes_dev, scales_dev, stream=0):
+    _sizes(rows, C, group_size)
     status = (_lib or load()).wfq_rms_norm_quantize(x_dev, ldx, residual_dev, ldr, gain_dev, eps, dtype, rows, C,
                                                     group_size, h_dev, ldh, codes_dev, scales_dev, stream)
     if status != WFQ_OK:
@@ -273,18 +281,21 @@ def wfq_rms_norm_quantize(x_dev, ldx, residual_dev, ldr, gain_dev, eps, dtype, r
 
 
 def wfq_quantize_rows(x_dev, ldx, dtype, rows, C, group_size, codes_dev, scales_dev, stream=0):
+    _sizes(rows, C, group_size)
     status = (_lib or load()).wfq_quantize_rows(x_dev, ldx, dtype, rows, C, group_size, codes_dev, scales_dev, stream)
     if status != WFQ_OK:
         _check(status, "wfq_quantize_rows")
 
 
 def wfq_dequantize_rows(codes_dev, scales_dev, rows, C, group_size, dtype, v_dev, ldv, stream=0):
+    _sizes(rows, C, group_size)
     status = (_lib or load()).wfq_dequantize_rows(codes_dev, scales_dev, rows, C, group_size, dtype, v_dev, ldv, stream)
     if status != WFQ_OK:
         _check(status, "wfq_dequantize_rows")
 
 
 def wfq_linear_create(C, K, group_size, gated=0):
+    _sizes(C, K, group_size)
     lin = ctypes.c_void_p()
     _check(load().wfq_linear_create(ctypes.byref(lin), C, K, group_size, int(gated)), "wfq_linear_create")
     return lin
@@ -303,10 +314,12 @@ def wfq_linear_set_epilogue(lin, bias_dev, act=WFQ_ACT_NONE):
 
 
 def wfq_linear_workspace_bytes(lin, rows):
+    _sizes(rows)
     return int(load().wfq_linear_workspace_bytes(lin, rows))
 
 
 def wfq_linear_set_workspace(lin, dev_ptr, nbytes, rows):
+    _sizes(rows)
     _check(load().wfq_linear_set_workspace(lin, dev_ptr, nbytes, rows), "wfq_linear_set_workspace")
 
 
@@ -315,12 +328,14 @@ def wfq_linear_prepare_weights(lin, w_dev, ldw, dtype, stream=0):
 
 
 def wfq_linear_forward(lin, x_dev, ldx, rows, residual_dev, ldr, y_dev, ldy, stream=0):
+    _sizes(rows)
     status = (_lib or load()).wfq_linear_forward(lin, x_dev, ldx, rows, residual_dev, ldr, y_dev, ldy, stream)
     if status != WFQ_OK:
         _check(status, "wfq_linear_forward")
 
 
 def wfq_linear_forward_codes(lin, codes_dev, scales_dev, rows, residual_dev, ldr, y_dev, ldy, stream=0):
+    _sizes(rows)
     status = (_lib or load()).wfq_linear_forward_codes(lin, codes_dev, scales_dev, rows, residual_dev, ldr, y_dev, ldy,
                                                        stream)
     if status != WFQ_OK:
@@ -520,6 +535,8 @@ def _rows_of(x, C, what):
     shape = x.shape
     assert x.is_cuda and shape and shape[-1] == C, what
     rows = x.numel() // C
+    if rows >> 31:
+        _sizes(rows)
     if x.is_contiguous() or rows == 0:
         return rows, C
     assert C == 1 or x.stride(-1) == 1, f"{what}: channels must be contiguous"
@@ -565,6 +582,8 @@ class QuantizedRows:
     def __init__(self, rows, C, group_size, device, shape=None):
         if _torch is None:
             _load_torch()
+        if (rows | C | group_size) >> 31:               # one of them is negative or does not fit
+            _sizes(rows, C, group_size)
         self.rows, self.C, self.group_size = rows, C, group_size
         self.shape = (rows, C) if shape is None else shape
         self.groups = 1 if group_size == 0 or group_size >= C else -(-C // group_size)
