@@ -392,7 +392,8 @@ wfq_status_t wfq_plan_destroy(wfq_plan_t *plan);
  *   x_dev, residual_dev  device, `dtype`, [rows][C] with leading dimensions ldx, ldr; residual_dev may be NULL
  *   gain_dev             device, fp32 [C]
  *   h_dev                device, `dtype`, leading dimension ldh, or NULL (always NULL without a residual); may be x_dev
- *                        or residual_dev itself with the same leading dimension, otherwise it overlaps neither
+ *                        or residual_dev itself with the same leading dimension (with another one it is refused),
+ *                        otherwise it overlaps neither
  */
 wfq_status_t wfq_rms_norm_quantize(const void *x_dev, long long ldx, const void *residual_dev, long long ldr,
                                    const float *gain_dev, float eps, wfq_dtype_t dtype, int rows, int C, int group_size,
@@ -448,7 +449,8 @@ wfq_status_t wfq_linear_prepare_weights(wfq_linear_t *lin, const void *w_dev, lo
 /*
  * y = the layer on x[rows][C] (quantized on the way), or on rows that are quantized already with the layer's C and group
  * size.  residual_dev may be NULL, or y_dev itself with the same leading dimension, otherwise it does not overlap y; nor
- * does y overlap x or the codes.
+ * does y overlap x or the codes (WFQ_ERR_INVALID_ARG where they begin at the same address, or where residual_dev is y_dev
+ * with another leading dimension; other overlaps are not seen).
  * WFQ_ERR_NOT_PREPARED without weights or workspace, WFQ_ERR_INVALID_ARG for more rows than the workspace is for.  One
  * layer must not be used from two threads at the same time.  wfq_linear_forward must not run on two streams, or in two
  * graphs, at the same time either: its calls share one workspace.  wfq_linear_forward_codes uses none of it and may.  The

@@ -608,7 +608,7 @@ def rms_norm_quantize(x, gain, eps=1e-6, group_size=128, residual=None, out=None
     """Root-mean-square norm of the rows of x (+ residual) as (QuantizedRows, h).
 
     x, residual: CUDA tensors [..., C] of one type (fp32, fp16, bf16); gain: fp32 [C].  h is the sum in x's type, written
-    to `out` where given (residual itself is allowed); without a residual it is x."""
+    to `out` where given (x or residual itself, or memory that overlaps neither); without a residual it is x."""
     torch = _torch or _load_torch()
     C, dtype = gain.numel(), x.dtype
     code, index = _CODES.get(dtype), x.get_device()
@@ -702,7 +702,7 @@ class Linear:
         return y, ldy, residual.data_ptr(), ldr
 
     def forward(self, x, residual=None, y=None):
-        """x [..., C] -> y [..., K] (+ residual, which may be y)."""
+        """x [..., C] -> y [..., K] (+ residual, which may be y).  y overlaps neither x nor, else, the residual."""
         assert x.dtype is self._in and x.get_device() == self.index, "x"
         rows, ldx = _rows_of(x, self.C, "x")
         y, ldy, res, ldr = self._outputs(x.shape[:-1], residual, y)

@@ -1451,11 +1451,14 @@ wfq_status_t bind(wfq_linear *l)
     return WFQ_OK;
 }
 
-wfq_status_t check_io(const wfq_linear *l, int rows, const void *residual, long long ldr, const void *y, long long ldy)
+wfq_status_t check_io(const wfq_linear *l, int rows, const void *in, const void *residual, long long ldr, const void *y,
+                      long long ldy)
 {
     const size_t e = elem_bytes(l->out_dtype);
     if (!y || ldy < l->K || misaligned(y, e)) return WFQ_ERR_INVALID_ARG;
     if (residual && (ldr < l->K || misaligned(residual, e))) return WFQ_ERR_INVALID_ARG;
+    // Outputs leave while other CTAs still read inputs; a residual is read where its output goes, if it lies there.
+    if (y == in || (y == residual && rows > 1 && ldy != ldr)) return WFQ_ERR_INVALID_ARG;
     if (rows > 0x7fffff00) return WFQ_ERR_UNSUPPORTED;
     if (((rows + 127LL) / 128) * ((l->Kz + 63LL) / 64) > 0x7fffffffLL) return WFQ_ERR_UNSUPPORTED;
     return WFQ_OK;
@@ -1607,7 +1610,7 @@ wfq_status_t wfq_linear_forward_codes(wfq_linear_t *l, const int8_t *codes_dev, 
     if (!l || rows < 0) return WFQ_ERR_INVALID_ARG;
     if (!l->prepared) return WFQ_ERR_NOT_PREPARED;
     if (rows == 0) return WFQ_OK;
-    wfq_status_t s = check_io(l, rows, residual_dev, ldr, y_dev, ldy);
+    wfq_status_t s = check_io(l, rows, codes_dev, residual_dev, ldr, y_dev, ldy);
     if (s != WFQ_OK) return s;
     if (!codes_dev || !scales_dev || misaligned(codes_dev, 32) || misaligned(scales_dev, 16)) return WFQ_ERR_INVALID_ARG;
     if ((s = bind(l)) != WFQ_OK) return s;
@@ -1621,7 +1624,7 @@ wfq_status_t wfq_linear_forward(wfq_linear_t *l, const void *x_dev, long long ld
     if (!l || rows < 0) return WFQ_ERR_INVALID_ARG;
     if (!l->prepared || !l->xq) return WFQ_ERR_NOT_PREPARED;
     if (rows == 0) return WFQ_OK;
-    wfq_status_t s = check_io(l, rows, residual_dev, ldr, y_dev, ldy);
+    wfq_status_t s = check_io(l, rows, x_dev, residual_dev, ldr, y_dev, ldy);
     if (s != WFQ_OK) return s;
     if (!x_dev || ldx < l->C || misaligned(x_dev, elem_bytes(l->in_dtype)) || rows > l->max_rows)
         return WFQ_ERR_INVALID_ARG;

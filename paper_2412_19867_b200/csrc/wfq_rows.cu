@@ -596,6 +596,8 @@ wfq_status_t wfq_rms_norm_quantize(const void *x_dev, long long ldx, const void 
     const size_t e = elem_bytes(dtype);
     if (!x_dev || !gain_dev || !codes_dev || !scales_dev || (h_dev && !residual_dev)) return WFQ_ERR_INVALID_ARG;
     if (ldx < C || (residual_dev && ldr < C) || (h_dev && ldh < C)) return WFQ_ERR_INVALID_ARG;
+    // in place only row onto row: a row that lands elsewhere may be another one's input
+    if (h_dev && rows > 1 && ((h_dev == x_dev && ldh != ldx) || (h_dev == residual_dev && ldh != ldr))) return WFQ_ERR_INVALID_ARG;
     if (misaligned(x_dev, e) || misaligned(residual_dev, e) || misaligned(h_dev, e) || misaligned(gain_dev, 4) ||
         misaligned(codes_dev, 32) || misaligned(scales_dev, 16))
         return WFQ_ERR_INVALID_ARG;
