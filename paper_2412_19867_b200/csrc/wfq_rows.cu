@@ -68,7 +68,7 @@ __device__ __forceinline__ float rstd_of(float sum, const RowsArgs &a)
     return rsqrtf(fmaf(sum, a.per_C, a.eps));      // two units in the last place, and the rounding of 1 / C
 }
 
-// Rows that registers do not hold.  One CTA per row, two passes over it; the second
+// Rows of more channels than 1024 threads take.  One CTA per row, two passes over it; the second
 // reads the first one's h where it was stored (h may be x or residual itself).
 template <typename T, bool NORM>
 __global__ void __launch_bounds__(256) rows_any_kernel(RowsArgs a)
@@ -198,7 +198,11 @@ template <int VEC, typename T> __device__ __forceinline__ void store(T *p, const
     else *p = Elem<T>::put(v[0]);
 }
 
-// Rows of up to 32768 channels, held in registers: one pass.  `tpr` threads (whole warps) have a row, thread t the
+// Rows of up to 32768 channels: one pass.  They are held in registers up to 4096 channels (8192 in fp32 and in calls of few
+// rows) but for a few words that single elements spill; beyond, 1024 threads have 64 registers each and spill 0 to 284 bytes
+// a thread up to 16384 channels and 116 (quantized) to 972 (fp32 norm with a residual) up to 32768, where two passes by
+// rows_any_kernel take longer all the same: 2000 x 32768 fp32 with a residual 431 against 597 us, bf16 218 against 606,
+// quantized alone 45 against 410.  `tpr` threads (whole warps) have a row, thread t the
 // vectors t, t + tpr, ... of VEC elements; a CTA has several short rows.  A group of gs = VEC * lanes channels (lanes a
 // power of two up to 32) lies in neighbouring lanes; other groups are joined in shared memory (`direct` 0).
 // Bound by memory and by issue slots (a dozen instructions per value) alike: CTAs walk over the rows and ask for the next
@@ -482,8 +486,12 @@ cudaError_t launch_rows_mode(const RowsArgs &a, int tpr, cudaStream_t stream, bo
 template <typename T, int VEC, int NV>
 cudaError_t launch_rows_size(const RowsArgs &a, int tpr, cudaStream_t stream, bool pdl)
 {
-    return tpr <= 256 ? launch_rows_mode<T, VEC, NV, 256>(a, tpr, stream, pdl)
-                      : launch_rows_mode<T, VEC, NV, 1024>(a, tpr, stream, pdl);
+    // what launch_rows_t gives rows of so few threads
+    constexpr bool narrow = VEC * NV == 8 || (VEC * NV == 16 && sizeof(T) == 2);
+    if constexpr (narrow) {
+        if (tpr <= 256) return launch_rows_mode<T, VEC, NV, 256>(a, tpr, stream, pdl);
+    }
+    return launch_rows_mode<T, VEC, NV, 1024>(a, tpr, stream, pdl);
 }
 
 bool aligned(const void *p, long long ld, size_t elem, size_t bytes)
