@@ -413,6 +413,10 @@ wfq_status_t wfq_dequantize_rows(const int8_t *codes_dev, const float *scales_de
  *   y[r][k] = act(z[r][k]) + residual[r][k]                                        k < K
  * or, gated, with weights of 2K rows (K gates, then K values):
  *   y[r][k] = act(z[r][k]) * z[r][K + k] + residual[r][k]
+ * GELU is z Phi(z), the form with erf.  SiLU and GELU have the relative accuracy of the fast exponential, 4 + 1.2 |z| and
+ * 12 + 0.75 z^2 units in the last place for negative z; SiLU is 0 below -88.7, GELU below -13.2.  A NaN stays NaN in every
+ * activation.  A group's sum times one of its scales has to fit fp32, which it does for values of x and of w up to
+ * 2.6e36 / (channels of a group).
  * y is rounded once to the output type.  Which kernel runs, and over how many CTAs the channels of a tile are split,
  * depends on the number of rows; the fp32 sums over groups are then formed in another order.  The same call gives the
  * same bits.

@@ -963,8 +963,9 @@ constexpr int DOT_THREADS = 256, DOT_WARPS = DOT_THREADS / 32, DOT_COLS = 4, DOT
 constexpr int DOT_MAX_ROWS = 8;
 constexpr int DOT_SMEM_MAX = 96 * 1024;
 // Values that a CTA quantizes for itself: what its registers keep without taking them from the products.  With twice as many
-// 2 x 4096 -> 4096 takes 10.7 us and 1 x 4096 8.5 us, against 8.7 and 8.0 us (the first through the row quantizer); every
-// CTA reading 4 rows of 8192 twice takes 46 us.  Where the host is the bound the quantizer's launch costs 2 us.
+// 2 x 4096 -> 4096 takes 10.6 us and 1 x 4096 8.4 us, against 8.5 and 7.9 us (the first through the row quantizer); one row of
+// 5120 -> 5120 11.5 against 10.4 us, 8192 -> 8192 16.0 against 14.2, 8192 -> 1024 5.3 against 5.6 (all replayed from a
+// graph); every CTA reading 4 rows of 8192 twice takes 46 us.  Where the host is the bound the quantizer's launch costs 2 us.
 constexpr int DOT_KEEP = 2;
 constexpr int DOT_QUANTIZE_MAX = 8 * DOT_THREADS * DOT_KEEP;
 

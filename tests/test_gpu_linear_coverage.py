@@ -99,3 +99,19 @@ def test_weights_far_apart():
     near.prepare(w)
     other.prepare(far)
     assert torch.equal(near.forward(x), other.forward(x))
+
+
+@pytest.mark.parametrize("large", ["x", "w"])
+@pytest.mark.parametrize("shape,rows", [(14004, 3), (12016, 9), (12064, 40), (11064, 40), (11128, 200), (13128, 40), (13256, 300), (22032, 9)])
+@pytest.mark.parametrize("C,gs", [(256, 128), (1024, 0)])
+def test_largest_values(C, gs, shape, rows, large):
+    """All codes 127 and values at 0.95 of the range that the header gives: the scaled sum of a group is just below 3.4e38."""
+    K, a, c = 70, 0.95 * 2.68e36 / (gs or C), 1e-28
+    x = torch.full((rows, C), a if large == "x" else c, device="cuda")
+    w = torch.full((K, C), c if large == "x" else a, device="cuda")
+    layer = b.Linear(C, K, gs, rows, "f32")
+    layer.prepare(w)
+    b.wfq_linear_set_debug_option(layer.lin, b.WFQ_DEBUG_GEMM_SHAPE, shape)
+    want, tol = ref.linear(*ref.quantize(x, gs), *ref.quantize(w, gs), gs)
+    for y in (layer.forward(x), layer.forward_codes(b.quantize_rows(x, gs))):
+        assert ((y.double().cpu() - want).abs() <= tol).all()
