@@ -115,3 +115,26 @@ def test_largest_values(C, gs, shape, rows, large):
     want, tol = ref.linear(*ref.quantize(x, gs), *ref.quantize(w, gs), gs)
     for y in (layer.forward(x), layer.forward_codes(b.quantize_rows(x, gs))):
         assert ((y.double().cpu() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("rows,C,K,parts", [(40_000, 65_536, 48, "x"), (70_000, 64, 32_768, "y"), (300, 1024, 2_200_000, "w"),
+                                            (2, 1024, 2_200_000, "w"), (20, 1024, 2_200_000, "w")])
+def test_more_than_2_to_31_elements(rows, C, K, parts):
+    """Codes of x, y or codes of the weights beyond 2^31 (the residual in place with y): the last rows and columns against a
+    layer of their own."""
+    gs = 128
+    layer = b.Linear(C, K, gs, rows, "bf16")
+    x = torch.randn((rows, C), device="cuda", generator=torch.Generator("cuda").manual_seed(1), dtype=torch.bfloat16)
+    w = torch.randn((K, C), device="cuda", generator=torch.Generator("cuda").manual_seed(2), dtype=torch.bfloat16)
+    y = torch.empty((rows, K), dtype=torch.bfloat16, device="cuda")
+    for i in range(0, rows, 4096):
+        y[i:i + 4096] = (torch.arange(K, device="cuda") % 13 - 6).bfloat16()
+    layer.prepare(w)
+    layer.forward(x, residual=y, y=y)
+    layer.check_status()
+    r, k = min(rows, 130), min(K, 140)
+    for rs in (slice(0, r), slice(rows - r, rows)):
+        for ks in (slice(0, k), slice(K - k, K)):
+            res = (torch.arange(K, device="cuda")[ks] % 13 - 6).bfloat16().expand(r, k).contiguous()
+            want, tol = ref.linear(*ref.quantize(x[rs], gs), *ref.quantize(w[ks], gs), gs, residual=res, dtype=torch.bfloat16)
+            assert ((y[rs, ks].double().cpu() - want).abs() <= tol).all()
